@@ -1,7 +1,8 @@
 /*
- * libsvf - the two per-token rules beside the sparse verification kernels, on AMD MI355X:
- * expert skipping of the sparse mixture of experts (Sec. 3.5, Eq. 15-16) and the acceptance /
- * resampling of the draft tokens (Sec. 2.1, Eq. 2-3).
+ * libsvf - the per-token rules beside the sparse verification kernels, on AMD MI355X:
+ * expert skipping of the sparse mixture of experts (Sec. 3.5, Eq. 15-16), the acceptance /
+ * resampling of the draft tokens (Sec. 2.1, Eq. 2-3), and sampling: the distributions that acceptance
+ * compares and the tokens drawn from them, from a model's logits.
  *
  * Conventions as in svf.h: every pointer is a DEVICE pointer owned by the caller unless said
  * otherwise; work is enqueued on `stream` and the call returns immediately; 0 on success, a
@@ -58,6 +59,33 @@ int svf_moe_calibrate(const float* w_cal, int32_t T, int32_t k, float* beta, voi
 int svf_accept_resample(const float* p_target, const float* p_draft, const int32_t* draft_tokens,
                         const float* u_accept, const float* u_resample, int32_t B, int32_t gamma, int32_t V,
                         int32_t* n_accepted, int32_t* resampled, void* stream);
+
+/* Bytes of device workspace svf_sample needs (multiple of 256; 0 if rows or V is out of range). */
+size_t svf_sample_workspace_bytes(int32_t rows, int32_t V);
+
+/*
+ * Sampling.  logits: [rows][V], element type dtype (SVF_F32 or SVF_BF16, svf.h), rows logits_stride
+ * elements apart (0: V); 1 <= V <= 524288.  Per row r, with its own settings (each array may be NULL: off for
+ * all rows):
+ *   temperature  fp32  weights w_v = exp((x_v - max x) / temperature).  A temperature that is not above zero takes the most
+ *                      likely token (temperature 1, top_k 1).
+ *   top_k        int32 keeps the k most likely tokens; off if <= 0
+ *   top_p        fp32  of these keeps the fewest, most likely first, whose weights reach top_p of their sum:
+ *                      a token stays if the ones in front of it have less.  Off if >= 1 or not a number; the first always stays.
+ *   min_p        fp32  drops tokens whose probability is below min_p times the largest (x_v < max x + temperature ln min_p); off
+ *                      if <= 0 or not a number
+ * "Most likely" orders equal logits by their index, lowest first.  Then, over the kept tokens,
+ *   tokens       int32 the first token (by index) up to which the kept weights sum to more than u[r] times
+ *                      their total; u: fp32, uniform numbers in [0, 1) supplied by the caller
+ *   probs        fp32  [rows][V], the kept weights over their total, zero elsewhere: what svf_accept_resample takes
+ * u and tokens are given both or not at all, and tokens or probs at least.  Logits of -inf (masked tokens) have
+ * weight zero, NaN counts as -inf; a row of nothing else gets token -1 and probabilities of zero.
+ * Weights are summed exactly, in fixed point with 43 fractional bits: the same bits from call to call.
+ */
+int svf_sample(const void* logits, int32_t dtype, int64_t logits_stride, int32_t rows, int32_t V,
+               const float* temperature_or_null, const int32_t* top_k_or_null, const float* top_p_or_null,
+               const float* min_p_or_null, const float* u_or_null, int32_t* tokens_or_null, float* probs_or_null,
+               void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

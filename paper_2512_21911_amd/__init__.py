@@ -12,7 +12,9 @@ from .binding import (NATIVE_CALLS, SVF_BF16, SVF_F32, SVF_STEP_ANCHOR, SVF_STEP
                       SVF_BUDGET_GLOBAL, SVF_BUDGET_PER_HEAD, SVF_GROUP_MAX, SVF_GROUP_MEAN, SVF_SUMMARY_MEAN,
                       SVF_SUMMARY_MINMAX, SvfRetrieval,
                       SVF_ACT_GELU, SVF_ACT_SILU, SVF_FFN_WALK_AUTO, SVF_FFN_WALK_GATE_FIRST, SVF_FFN_WALK_TOGETHER, SvfFfnShape, make_ffn_shape, new_ffn_workspace,
-                      svf_ffn_workspace_bytes, svf_moe_calibrate)
+                      svf_ffn_workspace_bytes, svf_moe_calibrate,
+                      SvfChunkShape, make_chunk_shape, new_chunk_workspace, svf_chunk_workspace_bytes, new_sample_workspace,
+                      svf_sample_workspace_bytes)
 
 __all__ = [n for n in globals() if not n.startswith("_")] + list(NATIVE_CALLS)
 

@@ -56,6 +56,21 @@ SVF_ACT_SILU, SVF_ACT_GELU = 0, 1
 SVF_FFN_WALK_AUTO, SVF_FFN_WALK_GATE_FIRST, SVF_FFN_WALK_TOGETHER = 0, 1, 2
 
 
+class SvfChunkShape(ctypes.Structure):
+    """Mirror of svf_chunk_shape_t (include/svf_cache.h)."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("max_new", ctypes.c_int32),
+        ("n_rows", ctypes.c_int32), ("window", ctypes.c_int32),
+        ("kv_stride_page", ctypes.c_int64), ("kv_stride_tok", ctypes.c_int64), ("kv_stride_head", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64),
+        ("sm_scale", ctypes.c_float), ("rotary_dim", ctypes.c_int32), ("rotary_interleaved", ctypes.c_int32),
+        ("rotary_scale", ctypes.c_float),
+    ]
+
+
 class SvfError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -70,7 +85,8 @@ EXPORTS = ["svf_version", "svf_strerror", "svf_budget_blocks", "svf_workspace_by
            "svf_mask_words", "svf_analytics_workspace_bytes", "svf_select_per_draft", "svf_masks_from_selection",
            "svf_overlap_by_distance", "svf_jaccard_adjacent", "svf_topk_anchors",
            "svf_block_summaries", "svf_retrieve", "svf_ffn_workspace_bytes", "svf_sparse_ffn",
-           "svf_moe_skip", "svf_moe_calibrate_workspace_bytes", "svf_moe_calibrate", "svf_accept_resample"]
+           "svf_moe_skip", "svf_moe_calibrate_workspace_bytes", "svf_moe_calibrate", "svf_accept_resample",
+           "svf_append_kv", "svf_chunk_workspace_bytes", "svf_chunk_attn", "svf_sample_workspace_bytes", "svf_sample"]
 
 
 def lib() -> ctypes.CDLL:
@@ -128,6 +144,17 @@ def lib() -> ctypes.CDLL:
         L.svf_moe_calibrate.argtypes = [vp, i32, i32, vp, vp, ctypes.c_size_t, vp]
         L.svf_accept_resample.restype = ctypes.c_int
         L.svf_accept_resample.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp]
+        csp = ctypes.POINTER(SvfChunkShape)
+        L.svf_append_kv.restype = ctypes.c_int
+        L.svf_append_kv.argtypes = [csp] + [vp] * 13
+        L.svf_chunk_workspace_bytes.restype = ctypes.c_size_t
+        L.svf_chunk_workspace_bytes.argtypes = [csp]
+        L.svf_chunk_attn.restype = ctypes.c_int
+        L.svf_chunk_attn.argtypes = [csp] + [vp] * 10 + [ctypes.c_size_t, vp]
+        L.svf_sample_workspace_bytes.restype = ctypes.c_size_t
+        L.svf_sample_workspace_bytes.argtypes = [i32, i32]
+        L.svf_sample.restype = ctypes.c_int
+        L.svf_sample.argtypes = [vp, i32, i64, i32, i32] + [vp] * 8 + [ctypes.c_size_t, vp]
         L.svf_version.argtypes = []
         L.svf_strerror.restype = ctypes.c_char_p
         L.svf_strerror.argtypes = [ctypes.c_int]
@@ -166,7 +193,8 @@ def _check(rc: int, where: str):
 # package is imported: loading it maps libsvf.so, and a program that imports the package to build the library must
 # not be left with the one that was there before.
 NATIVE_CALLS = ("svf_block_reps", "svf_score_select", "svf_verify_attn", "svf_verify_attn_static_ws", "svf_verify_step",
-                "svf_block_summaries", "svf_retrieve", "svf_sparse_ffn", "svf_moe_skip", "svf_accept_resample")
+                "svf_block_summaries", "svf_retrieve", "svf_sparse_ffn", "svf_moe_skip", "svf_accept_resample",
+                "svf_append_kv", "svf_chunk_attn", "svf_sample")
 
 
 def _native_calls():
@@ -175,7 +203,7 @@ def _native_calls():
         raise RuntimeError(f"{CALLS_PATH} is missing: build it with __graft_entry__.build() "
                            "or `python -m paper_2512_21911_amd.build`")
     from . import _svf_calls
-    _svf_calls.set_structures(SvfShape, SvfRetrieval, SvfFfnShape)
+    _svf_calls.set_structures(SvfShape, SvfRetrieval, SvfFfnShape, SvfChunkShape)
     return _svf_calls
 
 
@@ -346,3 +374,40 @@ def svf_moe_calibrate(w_cal, beta, ws=None):
     if ws is None:
         ws = torch.empty(int(lib().svf_moe_calibrate_workspace_bytes(T, k)), dtype=torch.uint8, device=w_cal.device)
     _check(lib().svf_moe_calibrate(_ptr(w_cal), T, k, _ptr(beta), _ptr(ws), ws.numel(), _stream()), "svf_moe_calibrate")
+
+
+# ---- filling the cache, attention of new tokens, sampling (argument marshalling only) -------------
+
+def make_chunk_shape(*, B, Hq, Hkv, d, dtype, max_seq_len, max_new, n_rows, n_pages, page_size=0, max_pages_per_seq=0,
+                     k_pool: Optional[torch.Tensor] = None, kv_strides=None, window=0, q_stride=0, k_stride=0, v_stride=0,
+                     out_stride=0, sm_scale=0.0, rotary_dim=0, rotary_interleaved=False, rotary_scale=0.0) -> SvfChunkShape:
+    """Fill an svf_chunk_shape_t.  The cache's strides come from `kv_strides` = (page, token, head) in elements,
+    or from a pool tensor laid out [page][slot][Hkv][d]."""
+    if kv_strides is None:
+        kv_strides = (k_pool.stride(0), k_pool.stride(1), k_pool.stride(2))
+    code = {torch.float32: SVF_F32, torch.bfloat16: SVF_BF16, "f32": SVF_F32, "bf16": SVF_BF16}.get(dtype, dtype)
+    return SvfChunkShape(B, Hq, Hkv, d, code, page_size, max_pages_per_seq, n_pages, max_seq_len, max_new, n_rows, window,
+                         kv_strides[0], kv_strides[1], kv_strides[2], q_stride, k_stride, v_stride, out_stride, sm_scale,
+                         rotary_dim, int(rotary_interleaved), rotary_scale)
+
+
+def svf_chunk_workspace_bytes(shape: SvfChunkShape) -> int:
+    return int(lib().svf_chunk_workspace_bytes(ctypes.byref(shape)))
+
+
+def new_chunk_workspace(shape: SvfChunkShape, device="cuda") -> torch.Tensor:
+    n = svf_chunk_workspace_bytes(shape)
+    if n == 0:
+        raise SvfError(-2, "svf_chunk_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def svf_sample_workspace_bytes(rows: int, V: int) -> int:
+    return int(lib().svf_sample_workspace_bytes(rows, V))
+
+
+def new_sample_workspace(rows: int, V: int, device="cuda") -> torch.Tensor:
+    n = svf_sample_workspace_bytes(rows, V)
+    if n == 0:
+        raise SvfError(-2, "svf_sample_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)

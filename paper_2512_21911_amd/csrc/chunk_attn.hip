@@ -1,0 +1,462 @@
+// Attention of new tokens over the cache in bf16 (svf_chunk_attn).
+#include <hip/hip_bf16.h>
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "svf_chunk_device.h"
+
+namespace svf {
+
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short shortx4;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kKeys = 64;                                // keys of a unit
+constexpr int kMostB = 4096;
+constexpr float kRescaleGap = 8.0f;                      // log2 units the maximum in use may lag behind
+
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const floatx2 f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+
+// One item: R query rows (row r = query head r % G of new token r / G) of a (sequence, KV head) against the
+// 64-key units they see.
+template <int R>
+struct Item {
+  int row0, rows, first, last, unit0, units;
+  __device__ __forceinline__ Item(const ChunkParams& p, const ChunkSeq& s, int i) {
+    const int M = s.n * p.G;
+    row0 = i * R;
+    rows = min(R, M - row0);
+    const int j0 = row0 / p.G, j1 = (row0 + rows - 1) / p.G;
+    first = p.window > 0 ? max(0, s.len + j0 + 1 - p.window) : 0;
+    last = s.len + j1;
+    unit0 = first / kKeys;
+    units = last / kKeys + 1 - unit0;
+  }
+};
+template <int R>
+__device__ __forceinline__ int items_of(const ChunkParams& p, const ChunkSeq& s) { return (s.n * p.G + R - 1) / R; }
+
+__device__ __forceinline__ ChunkSeq load_seq(const ChunkParams& p, int b) {
+  return chunk_seq(p.seq_lens[b], p.new_rows[b], p.new_lens[b], p.max_seq_len, p.max_new, p.n_rows);
+}
+
+__device__ __forceinline__ int64_t shfl_up64(int64_t x, int d) {
+  const int lo = __shfl_up((int)(x & 0xffffffff), d, 64), hi = __shfl_up((int)(x >> 32), d, 64);
+  return ((int64_t)hi << 32) | (uint32_t)lo;
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int l) {
+  const int lo = __builtin_amdgcn_readlane((int)(x & 0xffffffff), l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
+  return ((int64_t)hi << 32) | (uint32_t)lo;
+}
+__device__ __forceinline__ int64_t wave_scan64(int64_t x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t y = shfl_up64(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Units of all items of one KV head of a sequence, by a wavefront.
+template <int R>
+__device__ int64_t units_of_seq(const ChunkParams& p, const ChunkSeq& s, int lane) {
+  const int n = items_of<R>(p, s);
+  int64_t sum = 0;
+  for (int i = lane; i < n; i += 64) sum += Item<R>(p, s, i).units;
+  return lane64(wave_scan64(sum, lane), 63);
+}
+
+// How the work of a call is shared: all units of all items in a row (sequence, KV head, item, unit), cut into as many
+// equal ranges as there are workgroups.
+struct Cursor {
+  int b, h, item;            // where a range begins
+  int64_t skip;              // units of that item in front of it
+  int64_t total;
+};
+// cum: [kMostB + 1] in LDS
+template <int R>
+__device__ void units_before(const ChunkParams& p, int64_t* cum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = threadIdx.x; b < p.B; b += kThreads) {
+    const ChunkSeq s = load_seq(p, b);
+    const int n = items_of<R>(p, s);
+    cum[b + 1] = n == 0 ? 0 : n == 1 ? Item<R>(p, s, 0).units : -1;
+  }
+  __syncthreads();
+  for (int b = wave; b < p.B; b += kWaves) {
+    if (cum[b + 1] >= 0) continue;
+    const int64_t u = units_of_seq<R>(p, load_seq(p, b), lane);
+    if (lane == 0) cum[b + 1] = u;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int64_t run = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+      const int64_t x = wave_scan64(b0 + lane < p.B ? cum[b0 + lane + 1] * p.Hkv : 0, lane);
+      if (b0 + lane < p.B) cum[b0 + lane + 1] = run + x;
+      run += lane64(x, 63);
+    }
+    if (lane == 0) cum[0] = 0;
+  }
+  __syncthreads();
+}
+template <int R>
+__device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at) {
+  const int lane = threadIdx.x & 63;
+  Cursor c;
+  int lo = 0, hi = p.B - 1;                              // the last sequence with cum[b] <= at that has units
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (cum[mid] <= at) lo = mid;
+    else hi = mid - 1;
+  }
+  c.b = lo;
+  const int64_t of_seq = (cum[lo + 1] - cum[lo]) / p.Hkv;
+  int64_t rest = at - cum[lo];
+  c.h = (int)(rest / of_seq);
+  rest -= c.h * of_seq;
+  const ChunkSeq s = load_seq(p, c.b);
+  const int n = items_of<R>(p, s);
+  c.item = 0;
+  for (int i0 = 0;; i0 += 64) {
+    const int64_t x = wave_scan64(i0 + lane < n ? Item<R>(p, s, i0 + lane).units : 0, lane);
+    const uint64_t in = __ballot(rest < x);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      c.item = i0 + l;
+      if (l > 0) rest -= lane64(x, l - 1);
+      break;
+    }
+    rest -= lane64(x, 63);
+  }
+  c.skip = rest;
+  return c;
+}
+
+// The workspace: for every workgroup two partial results of R rows (0: of the item its range begins inside of, 1: of the one
+// its range ends inside of) and what the second launch joins.
+template <int D, int R>
+struct Parts {
+  float* o;                  // [N][2][R][D], relative to the maximum
+  float2* ml;                // [N][2][R] maximum (log2 units), denominator
+  int4* join;                // [N] of the item that begins in a range and ends behind it: b, KV head, item, last workgroup; b < 0: none
+  __host__ __device__ Parts(char* ws, int n) {
+    o = reinterpret_cast<float*>(ws);
+    ml = reinterpret_cast<float2*>(ws + (size_t)n * 2 * R * D * sizeof(float));
+    join = reinterpret_cast<int4*>(ws + (size_t)n * 2 * R * (D * sizeof(float) + sizeof(float2)));
+  }
+  static size_t bytes(int n) { return (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
+};
+
+template <int D, int RB>
+struct Kernel {
+  static constexpr int R = kWaves * 32 * RB;             // rows of an item
+  static constexpr int kRowBytes = 2 * D;
+  static constexpr int kChunks = D / 8;                  // sixteen-byte chunks of a row
+  static constexpr int kTileBytes = kKeys * kRowBytes;   // K or V of a unit
+  static constexpr int kRowsPerPass = kThreads / kChunks;
+  static constexpr int kPasses = kKeys / kRowsPerPass;
+  static constexpr int kLds = 4 * kTileBytes > (kMostB + 1) * 8 ? 4 * kTileBytes : (kMostB + 1) * 8;
+
+  // K chunk c of key t at c ^ (t mod 16) (d = 64, two rows to a line of banks: c ^ (t / 2 mod 8)): sixteen lanes that read the same chunk of
+  // sixteen keys hit all banks.
+  static __device__ __forceinline__ uint32_t k_at(int t, int c) {
+    return t * kRowBytes + ((c ^ (D == 128 ? t & 15 : (t >> 1) & 7)) << 4);
+  }
+  // V chunk c of key t at c ^ 4 (t mod 4) (d = 64: c ^ 4 (t / 2 mod 2) ): the four keys that sixteen lanes of a transposing read address
+  // lie in different banks.
+  static __device__ __forceinline__ uint32_t v_at(int t, int c) {
+    return t * kRowBytes + ((c ^ (D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1))) << 4);
+  }
+};
+
+template <int D, int RB>
+__global__ __launch_bounds__(kThreads, 1) void chunk_attn_kernel(ChunkParams p) {
+  typedef Kernel<D, RB> C;
+  constexpr int R = C::R;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hh = lane >> 5, r32 = lane & 31;
+  const int me = blockIdx.x;
+  const Parts<D, R> parts(p.ws, gridDim.x);
+
+  int64_t* const cum = reinterpret_cast<int64_t*>(lds);
+  units_before<R>(p, cum);
+  const int64_t total = cum[p.B];
+  const int N = (int)min((int64_t)gridDim.x, total);     // workgroups with work: one unit at least
+  if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
+  if (me >= N) return;
+  int64_t at = total * me / N;
+  const int64_t end = total * (me + 1) / N;
+  Cursor c = cursor_at<R>(p, cum, at);
+  __syncthreads();
+
+  const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
+  while (at < end) {
+    const ChunkSeq s = load_seq(p, c.b);
+    const Item<R> it(p, s, c.item);
+    const int n = (int)min((int64_t)it.units - c.skip, end - at);        // units of this item in the range
+    const int unit0 = it.unit0 + (int)c.skip;
+    const char* const K = static_cast<const char*>(p.K) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
+    const char* const V = static_cast<const char*>(p.V) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
+
+    const auto place = [&](int unit, int i) -> int64_t {                 // bytes from the pool's start
+      const int t = min(max(unit * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last);
+      if (p.kv.page_size == 0) return 2 * ((int64_t)c.b * p.kv.stride_page + (int64_t)t * p.kv.stride_tok);
+      const int np = p.kv.page_shift >= 0 ? t >> p.kv.page_shift : t / p.kv.page_size;
+      int page = p.table[(int64_t)c.b * p.kv.max_pages + np];
+      if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
+      return 2 * ((int64_t)page * p.kv.stride_page + (int64_t)(t - np * p.kv.page_size) * p.kv.stride_tok);
+    };
+    u32x4 kx[C::kPasses], vx[C::kPasses];
+    const auto request = [&](int unit) {
+#pragma unroll
+      for (int i = 0; i < C::kPasses; ++i) {
+        const int64_t off = place(unit, i);
+        kx[i] = *reinterpret_cast<const u32x4*>(K + off);
+        vx[i] = *reinterpret_cast<const u32x4*>(V + off);
+      }
+    };
+    const auto put = [&](int buf) {
+      char* const k = lds + buf * 2 * C::kTileBytes;
+      char* const v = k + C::kTileBytes;
+#pragma unroll
+      for (int i = 0; i < C::kPasses; ++i) {
+        const int t = t_lane + i * C::kRowsPerPass;
+        *reinterpret_cast<u32x4*>(k + C::k_at(t, c_lane)) = kx[i];
+        *reinterpret_cast<u32x4*>(v + C::v_at(t, c_lane)) = vx[i];
+      }
+    };
+    request(unit0);
+
+    // this lane's rows: r32 of each of the wavefront's RB blocks
+    bf16x8 qf[RB][D / 16];
+    int hi[RB], lo[RB];
+    floatx16 o[RB][D / 32] = {};
+    float m[RB], l[RB];
+    const bool rows_here = wave * 32 * RB < it.rows;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = it.row0 + min(wave * 32 * RB + 32 * rb + r32, it.rows - 1), j = r / p.G;
+      const char* qr = static_cast<const char*>(p.q) +
+                       2 * ((int64_t)(s.row + j) * p.q_stride + (int64_t)(c.h * p.G + r - j * p.G) * D) + 16 * hh;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qr + 32 * ks);
+      hi[rb] = s.len + j;
+      lo[rb] = p.window > 0 ? hi[rb] + 1 - p.window : 0;
+      m[rb] = -INFINITY;
+      l[rb] = 0.f;
+    }
+    // units whose keys every row of the item sees need no mask
+    const int hi_all = s.len + it.row0 / p.G, lo_all = p.window > 0 ? it.last + 1 - p.window : 0;
+
+    put(0);
+    if (n > 1) request(unit0 + 1);
+    __syncthreads();
+    for (int u = 0; u < n; ++u) {
+      const int key0 = (unit0 + u) * kKeys;
+      if (u + 1 < n) {
+        put((u + 1) & 1);
+        if (u + 2 < n) request(unit0 + u + 2);
+      }
+      if (rows_here) {
+        const char* const k = lds + (u & 1) * 2 * C::kTileBytes;
+        const char* const v = k + C::kTileBytes;
+        floatx16 sc[2][RB] = {};
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              sc[kk][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[rb][ks], sc[kk][rb], 0, 0, 0);
+          }
+        if (key0 + kKeys - 1 > hi_all || key0 < lo_all) {
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
+                if (key > hi[rb] || key < lo[rb]) sc[kk][rb][i] = -INFINITY;
+              }
+        }
+        bf16x8 pf[RB][4];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          float top = fmaxf(sc[0][rb][0], sc[1][rb][0]);
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[0][rb][i], sc[1][rb][i]));
+          top = halves_max(top) * p.scale_log2;
+          // (a row whose keys so far are all masked keeps -inf and weights of zero)
+          if (__ballot(top > m[rb] + kRescaleGap || (m[rb] == -INFINITY && top > m[rb]))) {
+            const float now = fmaxf(m[rb], top);
+            const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - now);
+            m[rb] = now;
+            l[rb] *= f;
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) o[rb][cb] *= f;
+          }
+          const float use = m[rb] == -INFINITY ? 0.f : m[rb];
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int b8 = 0; b8 < 2; ++b8) {
+              u32x4 w;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kk][rb][8 * b8 + 2 * i], p.scale_log2, -use));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kk][rb][8 * b8 + 2 * i + 1], p.scale_log2, -use));
+                l[rb] += x + y;
+                w[i] = pack_bf16(x, y);
+              }
+              pf[rb][2 * kk + b8] = __builtin_bit_cast(bf16x8, w);
+            }
+        }
+        // V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels 16 (g mod 2) + 4 x .. + 3 of key j of the
+        // four keys of its half, and receives channel lane mod 16 of those keys
+        const int vt = 4 * hh + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vb = 8 * (lane & 1);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int cb = 0; cb < D / 32; ++cb) {
+            shortx4 x[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
+            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[rb][kb], o[rb][cb], 0, 0, 0);
+          }
+      }
+      __syncthreads();
+    }
+
+    // this item's result, whole or a part
+    const bool begins = c.skip == 0, ends = c.skip + n == it.units;
+    const int slot = begins ? 1 : 0;
+    if (begins && !ends && tid == 0) {
+      const int64_t last_unit = at + it.units - 1;
+      parts.join[me] = make_int4(c.b, c.h, c.item, (int)(((last_unit + 1) * N - 1) / total));
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = wave * 32 * RB + 32 * rb + r32;
+      const float den = halves_sum(l[rb]);
+      if (r >= it.rows) continue;
+      if (begins && ends) {
+        const int row = it.row0 + r, j = row / p.G, head = c.h * p.G + row - j * p.G;
+        const float inv = 1.0f / den;
+        char* to = static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D) + 8 * hh;
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const u32x2 w = {pack_bf16(o[rb][cb][4 * g] * inv, o[rb][cb][4 * g + 1] * inv),
+                             pack_bf16(o[rb][cb][4 * g + 2] * inv, o[rb][cb][4 * g + 3] * inv)};
+            *reinterpret_cast<u32x2*>(to + 64 * cb + 16 * g) = w;
+          }
+        if (p.lse && hh == 0)
+          p.lse[(int64_t)(s.row + j) * p.Hq + head] = (m[rb] + log2f(den)) * 0.69314718055994530942f;
+      } else {
+        const int64_t at_part = (int64_t)(2 * me + slot) * R + r;
+        float* to = parts.o + at_part * D + 4 * hh;
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const floatx4 x = {o[rb][cb][4 * g], o[rb][cb][4 * g + 1], o[rb][cb][4 * g + 2], o[rb][cb][4 * g + 3]};
+            *reinterpret_cast<floatx4*>(to + 32 * cb + 8 * g) = x;
+          }
+        if (hh == 0) parts.ml[at_part] = make_float2(m[rb], den);
+      }
+    }
+
+    // the next item
+    at += n;
+    c.skip = 0;
+    if (++c.item == items_of<R>(p, s)) {
+      c.item = 0;
+      if (++c.h == p.Hkv) {
+        c.h = 0;
+        ++c.b;
+        while (at < end && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with units: at < end)
+      }
+    }
+  }
+}
+
+// Joins the parts of the items that were cut; workgroup v: the item that begins in range v.
+template <int D, int R>
+__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
+  const int N = gridDim.x, me = blockIdx.x;
+  const Parts<D, R> parts(p.ws, N);
+  const int4 join = parts.join[me];
+  if (join.x < 0) return;
+  const ChunkSeq s = load_seq(p, join.x);
+  const Item<R> it(p, s, join.z);
+  for (int i = threadIdx.x; i < it.rows * (D / 4); i += kThreads) {
+    const int r = i / (D / 4), ch = 4 * (i % (D / 4));
+    float top = parts.ml[(int64_t)(2 * me + 1) * R + r].x;
+    for (int v = me + 1; v <= join.w; ++v) top = fmaxf(top, parts.ml[(int64_t)(2 * v) * R + r].x);
+    float den = 0.f;
+    floatx4 x = {};
+    for (int v = me; v <= join.w; ++v) {
+      const int64_t at = (int64_t)(2 * v + (v == me ? 1 : 0)) * R + r;
+      const float2 ml = parts.ml[at];
+      const float f = __builtin_amdgcn_exp2f(ml.x - top);
+      den += f * ml.y;
+      x += f * *reinterpret_cast<const floatx4*>(parts.o + at * D + ch);
+    }
+    const int row = it.row0 + r, j = row / p.G, head = join.y * p.G + row - j * p.G;
+    const float inv = 1.0f / den;
+    const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+    *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch)) = w;
+    if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
+  }
+}
+
+constexpr int kWorkgroups = 256;
+
+template <int D, int RB>
+hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
+  typedef Kernel<D, RB> C;
+  hipLaunchKernelGGL((chunk_attn_kernel<D, RB>), dim3(kWorkgroups), dim3(kThreads), C::kLds, st, p);
+  hipLaunchKernelGGL((chunk_merge_kernel<D, C::R>), dim3(kWorkgroups), dim3(kThreads), 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t chunk_attn_workspace(const svf_chunk_shape_t& s) {
+  return s.d == 128 ? Parts<128, Kernel<128, 2>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64, 2>::R>::bytes(kWorkgroups);
+}
+
+hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st) {
+  return p.d == 128 ? launch_d<128, 2>(p, st) : launch_d<64, 2>(p, st);
+}
+
+}  // namespace svf

@@ -18,6 +18,7 @@
 #include <vector>
 
 #include "svf.h"
+#include "svf_cache.h"
 #include "svf_ffn.h"
 #include "svf_rules.h"
 
@@ -29,7 +30,7 @@ struct Failed {};                      // a Python error is set
 enum Kind : uint8_t { kShape, kTensor, kWorkspace, kInt, kNumber };
 
 // The ctypes structures (set_structures), in the order of this enumeration.
-enum Structure : uint8_t { kSvfShape, kSvfRetrieval, kSvfFfnShape, kStructures };
+enum Structure : uint8_t { kSvfShape, kSvfRetrieval, kSvfFfnShape, kSvfChunkShape, kStructures };
 PyTypeObject* structures[kStructures];
 
 struct Param {
@@ -197,6 +198,29 @@ Sizes sizes_of(const Signature& s, const Args& a, int i, int dims) {
   return r;
 }
 
+// The rows of a two-dimensional tensor whose element type a C entry point takes as an argument.
+struct Rows {
+  int32_t dtype, rows, columns;
+  int64_t stride;
+};
+Rows rows_of(const Signature& s, const Args& a, int i) {
+  if (!THPVariable_Check(a.obj[i])) {
+    PyErr_Format(PyExc_TypeError, "%s(): %s must be a tensor", s.where, s.params[i].name);
+    throw Failed{};
+  }
+  const at::Tensor& t = THPVariable_Unpack(a.obj[i]);
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1) || t.size(0) != (int32_t)t.size(0) || t.size(1) != (int32_t)t.size(1)) {
+    PyErr_Format(PyExc_ValueError, "%s(): %s must have 2 dimensions, its rows contiguous", s.where, s.params[i].name);
+    throw Failed{};
+  }
+  if (t.size(0) > 1 && t.stride(0) < t.size(1)) {
+    PyErr_Format(PyExc_ValueError, "%s(): the rows of %s overlap", s.where, s.params[i].name);
+    throw Failed{};
+  }
+  const int32_t dtype = t.scalar_type() == at::kFloat ? SVF_F32 : t.scalar_type() == at::kBFloat16 ? SVF_BF16 : -1;
+  return {dtype, (int32_t)t.size(0), (int32_t)t.size(1), t.size(0) > 1 ? t.stride(0) : 0};
+}
+
 template <typename Shape>
 const Shape* shape_of(const Args& a, int i) { return static_cast<const Shape*>(a.ptr[i]); }
 
@@ -306,10 +330,33 @@ SVF_CALL(svf_accept_resample,
          tensor("p_target"), tensor("p_draft"), tensor("draft_tokens"), tensor("u_accept"), tensor("u_resample"),
          tensor("n_accepted"), tensor("resampled"))
 
+SVF_CALL(svf_append_kv,
+         const auto* sh = shape_of<svf_chunk_shape_t>(a, 0); void* st = stream(); NoGil free;
+         rc = svf_append_kv(sh, a.ptr[1], a.ptr[2], I32(3), I32(4), I32(5), I32(6), a.ptr[7], a.ptr[8], a.ptr[9], a.ptr[10],
+                            static_cast<const double*>(a.ptr[11]), I32(12), st),
+         shape("shape", kSvfChunkShape), tensor("k_new"), tensor("v_new"), tensor("block_table"), tensor("seq_lens"),
+         tensor("new_rows"), tensor("new_lens"), tensor("K"), tensor("V"), tensor_or_none("q"), tensor_or_none("q_out"),
+         tensor_or_none("inv_freq"), tensor_or_none("positions"))
+
+SVF_CALL(svf_chunk_attn,
+         const auto* sh = shape_of<svf_chunk_shape_t>(a, 0); void* st = stream(); NoGil free;
+         rc = svf_chunk_attn(sh, a.ptr[1], a.ptr[2], a.ptr[3], I32(4), I32(5), I32(6), I32(7), a.ptr[8],
+                             static_cast<float*>(a.ptr[10]), WS(9), st),
+         shape("shape", kSvfChunkShape), tensor("q"), tensor("K"), tensor("V"), tensor("block_table"), tensor("seq_lens"),
+         tensor("new_rows"), tensor("new_lens"), tensor("out"), workspace("ws"), tensor_or_none("lse"))
+
+SVF_CALL(svf_sample,
+         const Rows d = rows_of(s, a, 0); void* st = stream(); NoGil free;
+         rc = svf_sample(a.ptr[0], d.dtype, d.stride, d.rows, d.columns, F32(4), I32(5), F32(6), F32(7), F32(1),
+                         static_cast<int32_t*>(a.ptr[2]), static_cast<float*>(a.ptr[8]), WS(3), st),
+         tensor("logits"), tensor("u"), tensor("tokens"), workspace("ws"), tensor_or_none("temperature"),
+         tensor_or_none("top_k"), tensor_or_none("top_p"), tensor_or_none("min_p"), tensor_or_none("probs"))
+
 // Which classes the shapes are instances of; the binding says so before it makes the first call.
 PyObject* set_structures_py(PyObject*, PyObject* args) {
   PyObject* c[kStructures];
-  if (!PyArg_ParseTuple(args, "O!O!O!", &PyType_Type, &c[0], &PyType_Type, &c[1], &PyType_Type, &c[2])) return nullptr;
+  if (!PyArg_ParseTuple(args, "O!O!O!O!", &PyType_Type, &c[0], &PyType_Type, &c[1], &PyType_Type, &c[2],
+                        &PyType_Type, &c[3])) return nullptr;
   for (int i = 0; i < kStructures; ++i) {
     Py_INCREF(c[i]);
     Py_XDECREF(reinterpret_cast<PyObject*>(structures[i]));
@@ -332,7 +379,8 @@ std::string doc_of(const Signature& s) {
 PyMethodDef methods[] = {SVF_METHOD(svf_block_reps), SVF_METHOD(svf_score_select), SVF_METHOD(svf_verify_attn),
                          SVF_METHOD(svf_verify_attn_static_ws), SVF_METHOD(svf_verify_step), SVF_METHOD(svf_block_summaries),
                          SVF_METHOD(svf_retrieve), SVF_METHOD(svf_sparse_ffn), SVF_METHOD(svf_moe_skip),
-                         SVF_METHOD(svf_accept_resample),
+                         SVF_METHOD(svf_accept_resample), SVF_METHOD(svf_append_kv), SVF_METHOD(svf_chunk_attn),
+                         SVF_METHOD(svf_sample),
                          {"set_structures", set_structures_py, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_svf_calls", nullptr, -1, methods};
@@ -343,7 +391,8 @@ PyMODINIT_FUNC PyInit__svf_calls(void) {
   // (in the order of `methods`)
   Signature* const all[] = {&sig_svf_block_reps, &sig_svf_score_select, &sig_svf_verify_attn, &sig_svf_verify_attn_static_ws,
                             &sig_svf_verify_step, &sig_svf_block_summaries, &sig_svf_retrieve, &sig_svf_sparse_ffn,
-                            &sig_svf_moe_skip, &sig_svf_accept_resample};
+                            &sig_svf_moe_skip, &sig_svf_accept_resample, &sig_svf_append_kv, &sig_svf_chunk_attn,
+                            &sig_svf_sample};
   static std::string docs[sizeof(all) / sizeof(all[0])];
   static_assert(Args::kMost >= 16, "arguments of svf_verify_step");
   for (size_t i = 0; i < sizeof(all) / sizeof(all[0]); ++i) {

@@ -1,0 +1,62 @@
+// Shared by the kernels of include/svf_cache.h (not part of the C ABI).
+#pragma once
+
+#include "svf_cache.h"
+#include "svf_device.h"
+
+namespace svf {
+
+struct ChunkParams {
+  KvLayout kv;
+  const void* q;
+  const void* K;
+  const void* V;
+  const int32_t* table;
+  const int32_t* seq_lens;
+  const int32_t* new_rows;
+  const int32_t* new_lens;
+  void* out;
+  float* lse;                // may be null
+  char* ws;
+  int64_t q_stride, out_stride;      // elements
+  int32_t B, Hq, Hkv, G, d, n_pages, max_seq_len, max_new, n_rows, window;
+  float scale_log2;          // sm_scale * log2(e)
+};
+
+struct AppendParams {
+  KvLayout kv;
+  const void* k_new;
+  const void* v_new;
+  const void* q;             // may be null
+  void* q_out;
+  void* K;
+  void* V;
+  const int32_t* table;
+  const int32_t* seq_lens;
+  const int32_t* new_rows;
+  const int32_t* new_lens;
+  const int32_t* positions;  // may be null
+  const double* inv_freq;
+  int64_t q_stride, k_stride, v_stride;   // elements
+  int32_t B, Hq, Hkv, d, n_pages, max_seq_len, max_new, n_rows, rotary_dim, interleaved;
+  float rotary_scale;
+};
+
+// The tokens a sequence takes part with: clamped to what the shape has room for, so that no
+// contents of the device arrays lead outside the tensors.
+struct ChunkSeq { int len, row, n; };                    // cached tokens in front, first row, new tokens
+__device__ __forceinline__ ChunkSeq chunk_seq(int len, int row, int n, int max_seq_len, int max_new, int n_rows) {
+  ChunkSeq s{len, row, min(n, max_new)};
+  if (len < 0 || row < 0 || row >= n_rows) s.n = 0;
+  else s.n = max(0, min(s.n, min(n_rows - row, max_seq_len - len)));
+  if (s.n == 0) s.len = s.row = 0;
+  return s;
+}
+
+hipError_t launch_append_kv(const AppendParams& p, int dtype, hipStream_t st);
+size_t chunk_attn_workspace(const svf_chunk_shape_t& s);
+hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st);
+size_t chunk_attn_f32_workspace(const svf_chunk_shape_t& s);
+hipError_t launch_chunk_attn_f32(const ChunkParams& p, hipStream_t st);
+
+}  // namespace svf
