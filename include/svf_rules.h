@@ -65,7 +65,7 @@ size_t svf_sample_workspace_bytes(int32_t rows, int32_t V);
 
 /*
  * Sampling.  logits: [rows][V], element type dtype (SVF_F32 or SVF_BF16, svf.h), rows logits_stride
- * elements apart (0: V); 1 <= V <= 524288.  Per row r, with its own settings (each array may be NULL: off for
+ * elements apart (0: V); 1 <= rows <= 65535, 1 <= V <= 524288.  Per row r, with its own settings (each array may be NULL: off for
  * all rows):
  *   temperature  fp32  weights w_v = exp((x_v - max x) / temperature).  A temperature that is not above zero takes the most
  *                      likely token (temperature 1, top_k 1).
