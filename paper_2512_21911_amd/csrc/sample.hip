@@ -3,8 +3,8 @@
 // All three filters keep a prefix of the tokens in descending order of their logits (ties by index), so what a row keeps
 // is two numbers, a border: the key of the last kept logit and the index of the last kept token with it.  Nothing is sorted
 // but the few tokens around it.  A row is cut into slices, and three launches find border and token:
-//   stats    a workgroup per slice reads its logits once, into registers: their maximum, the sum of their weights, and, if the row has a
-//            filter, a histogram of counts and weights over 1023 bins of logits below the maximum (and one for the rest).
+//   stats    a workgroup per slice reads its logits once, into registers: their maximum and the sum of their weights or, if the row has a
+//            filter, a histogram of counts and weights over 1023 bins of logits from the maximum down.
 //   gather   every workgroup adds up the row's histograms for itself and knows the bin the border is in; it reads its slice again only if
 //            it has tokens there, and writes those to the row's list (top-k: all from the top on, so that
 //            the mass that top-p takes its share of is at hand).
@@ -14,9 +14,11 @@
 // A row whose border bin has more tokens than the list (many equal logits, a top-k of thousands) is settled in the third launch by
 // radix selection over the whole row.
 //
-// Weights are fixed-point numbers relative to their slice's maximum, so that sums do not depend on their order; slices are brought to the row's
-// maximum by one factor each.  2^t is a table of 64 entries in 64 bits times a cubic: good to 2^-30, which an fp32 exponential (2^-23) is
-// not, and a hundred thousand borders of tokens wait for the target in between.
+// Weights.  Bins are a power of two of logits wide, at whole multiples of it, so a logit's bin and its place in the bin are exact in fp32.  A
+// weight is its bin's, 2^(-bin c) in fp64, times 2^(place c), place c < 0.046: a short polynomial in fp32 whose rounding is 2^-24 of the
+// excess over one.  That is good to 2^-27, which an fp32 exponential of the whole argument is not (2^-20 at 20 below the maximum), and a hundred
+// thousand tokens' borders wait for the target in between; and a histogram adds whole numbers, count and weight in one 64-bit word.
+// (With fp64 arithmetic per logit and separate words the first launch took 20.1 instead of 16.9 us for 64 rows of 129 280 fp32 logits.)
 // Bound: the logits, once from memory and, where the border's bin is gathered and the slice walked, again from the caches.
 #include <hip/hip_bf16.h>
 #include <hip/hip_runtime.h>
@@ -32,23 +34,24 @@ namespace svf {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kFraction = 43;                            // bits of a weight behind the point; 2^19 weights of one fit 63 bits
+constexpr int kFraction = 43;                            // bits of a weight behind the point; 2^19 weights of 1.05 fit 63 bits
+constexpr int kPlaceBits = 31;                           // of a weight relative to its bin's: at least one, below two
+constexpr int kCountAt = 47;                             // a histogram's word: 2^15 such weights, and above them how many
 constexpr int kBins = 1024;                              // the last: everything below the others
 constexpr int kList = 4096;                              // tokens around the border that are sorted
-constexpr int kTable = 64;
 constexpr double kLog2e = 1.4426950408889634074;
 
 struct SliceStats {
   float top;                 // largest logit; -inf: the slice has none above that
   int32_t n;                 // logits above -inf (rows with a filter)
-  uint64_t total;            // sum of the weights, relative to top
-  uint64_t above;            // of the tokens in bins above the list's
+  double total;              // weight of all of them, relative to the bin of top
+  uint64_t above;            // weight that the slice keeps without those in the list, relative to the row's first bin
 };
 enum { kEverything, kFromList, kSlow };                  // how the border is found
 struct RowPlan {
   float top;
   int32_t how, listed, k;    // k: top-k, 0 if it drops nothing
-  uint64_t limit, above;     // without top-k: the weight (relative to top) that the kept tokens reach, and what is above the list's bin
+  uint64_t limit, above;     // without top-k: the weight that the kept tokens reach, and what is above the list's bin
 };
 struct Border { uint32_t key; int32_t index; double inv_total; };     // inv_total: 1 / total weight of the kept tokens
 
@@ -64,8 +67,7 @@ struct SampleParams {
   float* probs;
   int32_t rows, V, slice, slices;
   SliceStats* stats;         // [rows][slices]
-  uint64_t* mass;            // [rows][slices][kBins]
-  uint32_t* count;           // [rows][slices][kBins]
+  uint64_t* bins;            // [rows][slices][kBins]: count << kCountAt | weight relative to the bin's
   uint64_t* list;            // [rows][kList]: ~key in the high half, index in the low one
   RowPlan* plan;             // [rows]
   Border* border;            // [rows]
@@ -109,8 +111,8 @@ __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(
 // ---- a row's settings ------------------------------------------------------------------------------
 
 struct Settings {
-  double to_log2;            // log2(e) / temperature
   float temperature, top_p, min_p, per_bin;              // per_bin: bins to a unit of the logits, a power of two
+  double bin_log2;           // log2 of the weight from one bin to the next
   int k;
   __device__ __forceinline__ Settings(const SampleParams& p, int r) {
     temperature = p.temperature ? p.temperature[r] : 1.f;
@@ -121,18 +123,27 @@ struct Settings {
       temperature = 1.f;
       k = 1;
     }
+    temperature = fmaxf(temperature, 0x1p-60f);
     if (k >= p.V || k < 0) k = 0;
     if (!(top_p < 1.f)) top_p = 1.f;
     if (!(min_p > 0.f)) min_p = 0.f;
-    to_log2 = kLog2e / (double)temperature;
-    // a bin is 1/32 of a logit wide, and of the temperature's power of two if that is lower (down to 2^-20): the 1023 bins reach 32
-    // logits, or 32 to 64 temperatures' worth, below the maximum
-    const int e = min(0, max(-15, (int)((__float_as_uint(temperature) >> 23) & 255) - 127));
+    // a bin is 1/32 of a logit wide, and of the temperature's power of two if that is lower: the 1023 bins reach 32 logits, or 16
+    // to 32 temperatures, below the maximum
+    const int e = min(0, (int)((__float_as_uint(temperature) >> 23) & 255) - 127);
     per_bin = __uint_as_float((uint32_t)(127 + 5 - e) << 23);
+    bin_log2 = kLog2e / (double)temperature / (double)per_bin;
   }
   __device__ __forceinline__ bool filtered() const { return k > 0 || top_p < 1.f || min_p > 0.f; }
-  // monotone, exact: a whole number
-  __device__ __forceinline__ float bin_of(float x) const { return floorf(fminf(fmaxf(x, -1e30f), 1e30f) * per_bin); }
+  // the bin's number (from the logits' zero up; whole) and the place in it, 0 <= place < 1: both exact
+  __device__ __forceinline__ float bin_of(float x, float& place) const {
+    const float at = fminf(fmaxf(x * per_bin, -3e38f), 3e38f), b = floorf(at);
+    place = at - b;
+    return b;
+  }
+  __device__ __forceinline__ float bin_of(float x) const {
+    float place;
+    return bin_of(x, place);
+  }
   __device__ __forceinline__ uint32_t least_key(float top) const {
     if (min_p == 0.f) return 0;
     const double least = (double)top + (double)temperature * log((double)min_p);
@@ -144,30 +155,57 @@ struct Settings {
 
 // ---- weights ---------------------------------------------------------------------------------------
 
-// table[i] = 2^(i / 64) 2^43
-__device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < kTable) table[threadIdx.x] = exp2((double)threadIdx.x / kTable + kFraction);
+// 2^(place bin_log2) - 1; z = bin_log2 ln 2 <= 1/32
+__device__ __forceinline__ float place_excess(float place, float z) {
+  const float x = place * z;
+  return x * (1.f + x * (0.5f + x * (1.f / 6.f + x * (1.f / 24.f))));
 }
-// 2^((x - top) to_log2), times 2^43, as a number whose rounding is left to the caller
-__device__ __forceinline__ double weight_real(float x, double top, double to_log2, const double* table) {
-  const double t = fmax(((double)x - top) * to_log2, -1200.0);
-  const double n = rint(t * kTable);
-  const float r = (float)(t - n * (1.0 / kTable)) * 0.69314718055994530942f;
-  const float q = r * (1.f + r * (0.5f + r * (1.f / 6.f)));
-  const int k = (int)n;
-  const double w = table[k & (kTable - 1)];
-  return ldexp(__builtin_fma(w, (double)q, w), k >> 6);
+__device__ __forceinline__ float place_factor(const Settings& set) { return (float)(set.bin_log2 * 0.69314718055994530942); }
+// the same in fixed point, the one included
+__device__ __forceinline__ uint32_t place_weight(float place, float z) {
+  return (1u << kPlaceBits) + (uint32_t)(place_excess(place, z) * (float)(1u << kPlaceBits));
 }
-__device__ __forceinline__ uint64_t weight(float x, double top, double to_log2, const double* table) {
-  constexpr double kShift = 4503599627370496.0;          // 2^52: the sum's low bits are the rounded whole number
-  const double w = weight_real(x, top, to_log2, table) + kShift;
-  return __builtin_bit_cast(uint64_t, w) - __builtin_bit_cast(uint64_t, kShift);
+// 2^t, t <= 0: ten terms of the series around the nearest whole number, 2^-36 relative
+__device__ __forceinline__ double exp2_series(double t) {
+  t = fmax(t, -1200.0);
+  const double n = rint(t), x = (t - n) * 0.69314718055994530942;
+  double y = 1.0 / 362880;
+  y = __builtin_fma(y, x, 1.0 / 40320);
+  y = __builtin_fma(y, x, 1.0 / 5040);
+  y = __builtin_fma(y, x, 1.0 / 720);
+  y = __builtin_fma(y, x, 1.0 / 120);
+  y = __builtin_fma(y, x, 1.0 / 24);
+  y = __builtin_fma(y, x, 1.0 / 6);
+  y = __builtin_fma(y, x, 0.5);
+  y = __builtin_fma(y, x, 1.0);
+  y = __builtin_fma(y, x, 1.0);
+  return ldexp(y, (int)n);
 }
-// from a slice's maximum to the row's
-__device__ __forceinline__ double factor_of(float top, float row_top, double to_log2) {
-  return top == -INFINITY ? 0.0 : exp2(fmax(((double)top - (double)row_top) * to_log2, -1000.0));
+// weight of the lower end of the bin that lies b bins (a whole number, any size) below the first
+__device__ __forceinline__ double bin_weight(float b, const Settings& set) { return exp2_series(-(double)b * set.bin_log2); }
+// (below the 1024 bins: e^-16 and less at temperatures up to two, which an fp32 exponential does)
+__device__ __forceinline__ double rest_weight(float b, const Settings& set) {
+  return set.temperature <= 2.f ? (double)__builtin_amdgcn_exp2f(fmaxf((float)set.bin_log2 * -b, -1200.f)) : bin_weight(b, set);
 }
-__device__ __forceinline__ uint64_t scaled(uint64_t mass, double factor) { return (uint64_t)((double)mass * factor); }
+constexpr double kPlaceToRow = (double)(1u << (kFraction - kPlaceBits));
+
+// All weights of a row, relative to the bin of its maximum: table[b] = bin_weight(b) 2^(kFraction - kPlaceBits)
+struct Weights {
+  const double* table;
+  float first, z;
+  __device__ __forceinline__ Weights(const Settings& set, float top, const double* t)
+      : table(t), first(set.bin_of(top)), z(place_factor(set)) {}
+  static __device__ __forceinline__ void fill(const Settings& set, double* table) {
+    for (int b = threadIdx.x; b < kBins; b += blockDim.x) table[b] = bin_weight((float)b, set) * kPlaceToRow;
+  }
+  __device__ __forceinline__ uint64_t operator()(const Settings& set, float x) const {
+    float place;
+    const float b = first - set.bin_of(x, place);
+    constexpr double kShift = 4503599627370496.0;        // 2^52: the sum's low bits are the rounded whole number
+    const double w = (b < (float)kBins ? table[(int)b] : rest_weight(b, set) * kPlaceToRow) * (double)place_weight(place, z) + kShift;
+    return __builtin_bit_cast(uint64_t, w) - __builtin_bit_cast(uint64_t, kShift);
+  }
+};
 // the weight that the kept tokens reach, of `mass`
 __device__ __forceinline__ uint64_t limit_of(float top_p, uint64_t mass) {
   const double share = ceil((double)top_p * (double)mass);
@@ -176,57 +214,95 @@ __device__ __forceinline__ uint64_t limit_of(float top_p, uint64_t mass) {
 
 // ---- sums over a wavefront and a workgroup ---------------------------------------------------------
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t x, int d) { return __shfl_up((unsigned long long)x, d, 64); }
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) x += __shfl_xor((unsigned long long)x, d, 64);
+// (moves inside a row of sixteen lanes and from row to row: no trips through LDS)
+template <int CTRL, int ROWS, bool BOUND>
+__device__ __forceinline__ uint64_t lane_move64(uint64_t x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, BOUND);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, BOUND);
+  return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
+  x += lane_move64<0x111, 0xf, true>(x);    // row_shr:1
+  x += lane_move64<0x112, 0xf, true>(x);    // row_shr:2
+  x += lane_move64<0x114, 0xf, true>(x);    // row_shr:4
+  x += lane_move64<0x118, 0xf, true>(x);    // row_shr:8
+  x += lane_move64<0x142, 0xa, false>(x);   // row_bcast:15 -> rows 1, 3
+  x += lane_move64<0x143, 0xc, false>(x);   // row_bcast:31 -> rows 2, 3
   return x;
 }
-__device__ __forceinline__ uint64_t wave_scan64(uint64_t x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint64_t y = shfl_up64(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+__device__ __forceinline__ uint64_t lane64(uint64_t x, int l) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), l);
+  return (uint64_t)hi << 32 | lo;
 }
-// inclusive; every thread also gets the total.  sh: kWaves words, free when the call begins
-__device__ __forceinline__ uint64_t block_scan64(uint64_t x, uint64_t* sh, uint64_t& total) {
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t x) { return lane64(wave_scan64(x), 63); }
+// Inclusive scans of N numbers over the workgroup; every thread also gets the totals.  sh: N * kWaves words, free when the call begins.
+template <int N>
+__device__ __forceinline__ void block_scan64(uint64_t (&x)[N], uint64_t (&total)[N], uint64_t* sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  x = wave_scan64(x, lane);
-  if (lane == 63) sh[wave] = x;
-  __syncthreads();
-  uint64_t before = 0;
-  total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) before = total;
-    total += sh[w];
+  for (int i = 0; i < N; ++i) {
+    x[i] = wave_scan64(x[i]);
+    if (lane == 63) sh[i * kWaves + wave] = x[i];
   }
   __syncthreads();
-  return before + x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t upto = wave_scan64(lane < kWaves ? sh[i * kWaves + lane] : 0);
+    total[i] = lane64(upto, kWaves - 1);
+    if (wave > 0) x[i] += lane64(upto, __builtin_amdgcn_readfirstlane(wave) - 1);
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ uint64_t block_scan64(uint64_t x, uint64_t* sh, uint64_t& total) {
+  uint64_t a[1] = {x}, t[1];
+  block_scan64<1>(a, t, sh);
+  total = t[0];
+  return a[0];
+}
+__device__ __forceinline__ float wave_max(float x) {
+#define SVF_MAX(CTRL, ROWS) \
+  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, ROWS, 0xf, false)))
+  SVF_MAX(0x111, 0xf);
+  SVF_MAX(0x112, 0xf);
+  SVF_MAX(0x114, 0xf);
+  SVF_MAX(0x118, 0xf);
+  SVF_MAX(0x142, 0xa);
+  SVF_MAX(0x143, 0xc);
+#undef SVF_MAX
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ __forceinline__ float block_max(float x, float* sh) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) x = fmaxf(x, __shfl_xor(x, d, 64));
+  x = wave_max(x);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
   __syncthreads();
+  x = wave_max((threadIdx.x & 63) < kWaves ? sh[threadIdx.x & 63] : -INFINITY);
+  __syncthreads();
+  return x;
+}
+// (of a wavefront's lanes in a fixed order, then of the wavefronts')
+__device__ __forceinline__ double block_sum(double x, double* sh) {
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) x = fmaxf(x, sh[w]);
+  for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) x += sh[w];
   __syncthreads();
   return x;
 }
 
 // ---- stats -----------------------------------------------------------------------------------------
 
+constexpr uint64_t kWeightMask = (1ull << kCountAt) - 1;
+
 // grid: (slices, rows).  EPT: logits of a thread, four at a time
 template <typename T, int EPT>
 __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) {
-  __shared__ unsigned long long mass[kBins];
-  __shared__ uint32_t count[kBins];
-  __shared__ double table[kTable];
+  __shared__ uint64_t shared[kBins];                     // the histogram, or the bins' weights
   __shared__ float shf[kWaves];
-  __shared__ uint64_t sh[kWaves];
+  __shared__ double shd[kWaves];
+  __shared__ uint32_t all;
   const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int v0 = s * p.slice, end = min(v0 + p.slice, p.V);
@@ -234,60 +310,60 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
 #pragma unroll
   for (int i = 0; i < EPT / 4; ++i) f[i] = logits4(x, v0 + 4 * (i * kThreads + tid), end);
   const Settings set(p, r);
-  fill_table(table);
-  mass[tid] = 0;
-  count[tid] = 0;
+  const bool filtered = set.filtered();
+  unsigned long long* const bins = reinterpret_cast<unsigned long long*>(shared);
+  double* const table = reinterpret_cast<double*>(shared);
+  if (filtered) bins[tid] = 0;
+  else table[tid] = bin_weight((float)tid, set);
+  if (tid == 0) all = 0;
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EPT / 4; ++i) top = fmaxf(top, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
   top = block_max(top, shf);
-  const int64_t at = (int64_t)r * p.slices + s;
-  uint64_t total = 0;
+  const float first = set.bin_of(top), z = place_factor(set);
+  double total = 0.0;
   uint32_t n = 0;
-  const bool filtered = set.filtered();
   if (top > -INFINITY) {
-    const float first = set.bin_of(top);
-    uint64_t rest = 0;
-#pragma unroll
-    for (int i = 0; i < EPT / 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float l = get(f[i], e);
-        if (l == -INFINITY) continue;
-        const uint64_t w = weight(l, (double)top, set.to_log2, table);
-        const float b = first - set.bin_of(l);
-        if (filtered && b < kBins - 1) {
-          atomicAdd(&mass[(int)b], (unsigned long long)w);
-          atomicAdd(&count[(int)b], 1u);
-        } else {
-          rest += w;
-          ++n;
-        }
-      }
     if (filtered) {
-      rest = wave_sum64(rest);
 #pragma unroll
-      for (int d = 32; d > 0; d /= 2) n += __shfl_xor(n, d, 64);
-      if ((tid & 63) == 0) {
-        atomicAdd(&mass[kBins - 1], (unsigned long long)rest);
-        atomicAdd(&count[kBins - 1], n);
-      }
-      __syncthreads();
-      rest = mass[tid];
-      n = count[tid];
+      for (int i = 0; i < EPT / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float l = get(f[i], e);
+          float place;
+          const float b = first - set.bin_of(l, place);
+          n += l > -INFINITY;
+          if (b < (float)kBins) atomicAdd(&bins[(int)b], 1ull << kCountAt | place_weight(place, z));
+          else if (l > -INFINITY) total += rest_weight(b, set) * (1.0 + place_excess(place, z));
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float l = get(f[i], e);
+          float place;
+          const float b = first - set.bin_of(l, place);
+          const double q = 1.0 + place_excess(place, z);
+          if (b < (float)kBins) total += table[(int)b] * q;
+          else if (l > -INFINITY) total += rest_weight(b, set) * q;
+        }
     }
-    block_scan64(rest, sh, total);
   }
+  const int64_t at = (int64_t)r * p.slices + s;
   if (filtered) {
-    p.mass[at * kBins + tid] = top > -INFINITY ? mass[tid] : 0;
-    p.count[at * kBins + tid] = n;
-    uint64_t all;
-    block_scan64(n, sh, all);
-    n = (uint32_t)all;
+    __syncthreads();
+    const uint64_t word = bins[tid];
+    p.bins[at * kBins + tid] = word;
+    total += (double)(word & kWeightMask) * (1.0 / (double)(1u << kPlaceBits)) * bin_weight((float)tid, set);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) n += __shfl_xor(n, d, 64);
+    if ((tid & 63) == 0) atomicAdd(&all, n);
   }
+  total = block_sum(total, shd);
   if (tid == 0) {
     p.stats[at].top = top;
-    p.stats[at].n = (int)n;
+    p.stats[at].n = (int)all;
     p.stats[at].total = total;
   }
 }
@@ -296,72 +372,76 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
 
 constexpr int kMostSlices = 128;
 
-// Bins of the row, counted from its maximum's bin: `shift` bins of a slice further down than the slice's own.
+// Bins from the row's first down to the slice's first; kBins: none of the slice's is among the row's.
 __device__ __forceinline__ int shift_of(const Settings& set, float top, float row_top) {
   return top == -INFINITY ? kBins : (int)fminf(set.bin_of(row_top) - set.bin_of(top), (float)kBins);
+}
+// a slice's total relative to the row's first bin, in fixed point
+__device__ __forceinline__ uint64_t total_of(const SliceStats& st, const Settings& set, float row_top) {
+  if (st.top == -INFINITY) return 0;
+  return (uint64_t)(st.total * bin_weight(set.bin_of(row_top) - set.bin_of(st.top), set) * (double)(1ull << kFraction));
 }
 
 // grid: (slices, rows)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p) {
-  __shared__ uint64_t sh[kWaves];
-  __shared__ float tops[kMostSlices];
-  __shared__ double factor[kMostSlices];
+  __shared__ uint64_t sh[4 * kWaves];
   __shared__ int shift[kMostSlices];
+  __shared__ float shf[kWaves];
   __shared__ int k_bin, p_bin;
   __shared__ uint64_t upto_n, bin_n, above_m;
   __shared__ uint32_t used;
   const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
-  const Settings set(p, r);
   const int64_t row = (int64_t)r * p.slices;
-  if (tid < p.slices) tops[tid] = p.stats[row + tid].top;
+  SliceStats st{-INFINITY, 0, 0.0, 0};
+  if (tid < p.slices) st = p.stats[row + tid];
+  const Settings set(p, r);
   if (tid == 0) {
-    k_bin = p_bin = kBins - 1;
+    k_bin = p_bin = kBins;
     used = 0;
     upto_n = bin_n = above_m = 0;
   }
-  __syncthreads();
-  float top = -INFINITY;
-  for (int i = 0; i < p.slices; ++i) top = fmaxf(top, tops[i]);
+  const float top = block_max(st.top, shf);
+  const uint64_t whole = tid < p.slices && top > -INFINITY ? total_of(st, set, top) : 0;
   if (!set.filtered() || top == -INFINITY) {
     if (s == 0 && tid == 0) p.plan[r] = RowPlan{top, kEverything, 0, 0, 0, 0};
+    if (tid == s) p.stats[row + s].above = whole;
     return;
   }
-  uint64_t sum = 0, some = 0, total, n_finite;
-  if (tid < p.slices) {
-    factor[tid] = factor_of(tops[tid], top, set.to_log2);
-    shift[tid] = shift_of(set, tops[tid], top);
-    sum = scaled(p.stats[row + tid].total, factor[tid]);
-    some = (uint32_t)p.stats[row + tid].n;
+  if (tid < p.slices) shift[tid] = shift_of(set, st.top, top);
+  __syncthreads();
+  // thread b: bin b of the row (what slices hold further down is in none of them)
+  uint64_t mine = 0, m = 0, n = 0;
+#pragma unroll 4
+  for (int i = 0; i < p.slices; ++i) {
+    const int b = tid - shift[i];
+    const uint64_t w = b >= 0 ? p.bins[(row + i) * kBins + b] : 0;
+    n += w >> kCountAt;
+    m += w & kWeightMask;
+    if (i == s) mine = w & kWeightMask;
   }
-  block_scan64(sum, sh, total);
-  block_scan64(some, sh, n_finite);
-  const int k = (uint64_t)set.k < n_finite ? set.k : 0;
+  const double to_row = bin_weight((float)tid, set) * kPlaceToRow;
+  m = (uint64_t)((double)m * to_row);
+  uint64_t sums[4] = {n, m, whole, (uint64_t)(uint32_t)st.n}, totals[4];
+  block_scan64<4>(sums, totals, sh);
+  const uint64_t n_upto = sums[0], m_upto = sums[1];
+  const int k = (uint64_t)set.k < totals[3] ? set.k : 0;
   if (k == 0 && set.top_p == 1.f && set.min_p == 0.f) {
     if (s == 0 && tid == 0) p.plan[r] = RowPlan{top, kEverything, 0, 0, 0, 0};
+    if (tid == s) p.stats[row + s].above = whole;
     return;
   }
-  // thread b: bin b of the row
-  uint64_t m = 0, n = 0, all;
-  if (tid < kBins - 1)
-    for (int i = 0; i < p.slices; ++i) {
-      const int b = tid - shift[i];
-      if (b < 0) continue;
-      n += p.count[(row + i) * kBins + b];
-      m += scaled(p.mass[(row + i) * kBins + b], factor[i]);
-    }
-  const uint64_t n_upto = block_scan64(n, sh, all), m_upto = block_scan64(m, sh, all);
-  const uint64_t limit = limit_of(set.top_p, total);
+  const uint64_t limit = limit_of(set.top_p, totals[2]);
   if (k > 0) {
     if (n_upto >= (uint64_t)k && n_upto - n < (uint64_t)k) k_bin = tid;
   } else if (set.top_p < 1.f) {
     if (m_upto >= limit && m_upto - m < limit) p_bin = tid;
   }
   __syncthreads();
+  // the border's bin; kBins: below them all
   int hi = k > 0 ? k_bin : p_bin;
   if (k == 0 && set.min_p > 0.f) {
-    const float b = set.bin_of(top) - set.bin_of(key_logit(set.least_key(top)));
-    const int m_bin = (int)fminf(b, (float)(kBins - 1));
+    const int m_bin = (int)fminf(set.bin_of(top) - set.bin_of(key_logit(set.least_key(top))), (float)kBins);
     hi = set.top_p < 1.f ? min(hi, m_bin) : m_bin;
   }
   const int lo = k > 0 ? 0 : hi;
@@ -372,38 +452,34 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
   }
   __syncthreads();
   const uint64_t listed = k > 0 ? upto_n : bin_n;
-  const bool slow = hi == kBins - 1 || listed > kList;
+  const bool slow = hi == kBins || listed > kList;
   if (s == 0 && tid == 0)
     p.plan[r] = RowPlan{top, slow ? kSlow : kFromList, (int)listed, k, limit, k > 0 ? 0 : above_m};
   if (slow) return;
-  // this slice's tokens in the list's bins and above them, and those of the slices in front of it
-  uint64_t front_mine = 0, above = 0;
+  // this slice's tokens in the list's bins, those of the slices in front of it, and what it has above the list's bins
+  uint64_t parts[2] = {0, tid < lo ? (uint64_t)((double)mine * to_row) : 0}, of[2];
   if (tid >= lo && tid <= hi)
     for (int i = 0; i <= s; ++i) {
       const int b = tid - shift[i];
       if (b < 0) continue;
-      const uint64_t c = p.count[(row + i) * kBins + b];
-      front_mine += i == s ? c << 32 : c;
+      const uint64_t c = p.bins[(row + i) * kBins + b] >> kCountAt;
+      parts[0] += i == s ? c << 32 : c;
     }
-  if (tid < lo - shift[s]) above = p.mass[(row + s) * kBins + tid];
-  uint64_t counts;
-  block_scan64(front_mine, sh, counts);
-  block_scan64(above, sh, all);
-  if (tid == 0) p.stats[row + s].above = all;
-  if ((counts >> 32) == 0) return;
+  block_scan64<2>(parts, of, sh);
+  if (tid == 0) p.stats[row + s].above = of[1];
+  if ((of[0] >> 32) == 0) return;
   uint64_t* const list = p.list + (int64_t)r * kList;
-  const uint32_t list_at = (uint32_t)counts;             // (the histogram's count of what this slice adds)
+  const uint32_t list_at = (uint32_t)of[0];              // (the slice adds as many as the histogram says)
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int end = min((s + 1) * p.slice, p.V);
   const float first = set.bin_of(top);
+#pragma unroll 4
   for (int v = s * p.slice + 4 * tid; v < end; v += 4 * kThreads) {
     const float4 f = logits4(x, v, end);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float l = get(f, e);
-      if (l == -INFINITY) continue;
-      const float b = first - set.bin_of(l);
-      if (b >= (float)lo && b <= (float)hi) {
+      const float l = get(f, e), b = first - set.bin_of(l);
+      if (l > -INFINITY && b >= (float)lo && b <= (float)hi) {
         const uint32_t to = list_at + atomicAdd(&used, 1u);
         if (to < kList) list[to] = ((uint64_t)~score_key(l) << 32) | (uint32_t)(v + e);
       }
@@ -416,8 +492,8 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
 // Radix selection over the whole row: the largest key such that the tokens with keys above it have less than `limit` (of count, or
 // weight) and those with it and above have at least that; `before`: what those above have.
 template <typename T, bool WEIGHT>
-__device__ uint32_t select_key(const T* x, int V, float top, double to_log2, const double* table, uint64_t limit,
-                               unsigned long long* hist, uint64_t* sh, uint64_t& before) {
+__device__ uint32_t select_key(const T* x, int V, const Settings& set, const Weights& weight, uint64_t limit, unsigned long long* hist,
+                               uint64_t* sh, uint64_t& before) {
   uint32_t prefix = 0;
   before = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
@@ -428,7 +504,7 @@ __device__ uint32_t select_key(const T* x, int V, float top, double to_log2, con
       const float f = clean(load1(x + v));
       const uint32_t key = score_key(f);
       if ((key & hi_mask) == prefix)
-        atomicAdd(&hist[(key >> shift) & 255], WEIGHT ? (unsigned long long)weight(f, (double)top, to_log2, table) : 1ull);
+        atomicAdd(&hist[(key >> shift) & 255], WEIGHT ? (unsigned long long)weight(set, f) : 1ull);
     }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -451,13 +527,13 @@ __device__ uint32_t select_key(const T* x, int V, float top, double to_log2, con
 
 // The border of a row from all its logits.
 template <typename T>
-__device__ void slow_border(const T* x, int V, const Settings& set, int k, float top, const double* table, unsigned long long* hist,
+__device__ void slow_border(const T* x, int V, const Settings& set, int k, float top, const Weights& weight, unsigned long long* hist,
                             uint64_t* sh, uint32_t& key, int& index) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   key = 0;
   uint64_t ties = (uint64_t)V, before;
   if (k > 0) {
-    key = select_key<T, false>(x, V, top, set.to_log2, table, (uint64_t)k, hist, sh, before);
+    key = select_key<T, false>(x, V, set, weight, (uint64_t)k, hist, sh, before);
     ties = (uint64_t)k - before;
   }
   if (set.top_p < 1.f) {
@@ -465,16 +541,16 @@ __device__ void slow_border(const T* x, int V, const Settings& set, int k, float
     for (int v = tid; v < V; v += kThreads) {
       const float f = clean(load1(x + v));
       const uint32_t kf = score_key(f);
-      if (kf > key) mass += weight(f, (double)top, set.to_log2, table);
+      if (kf > key) mass += weight(set, f);
       same += kf == key;
     }
     block_scan64(mass, sh, all);
     mass = all;
     block_scan64(same, sh, all);
-    if (k > 0) mass += min(ties, all) * weight(key_logit(key), (double)top, set.to_log2, table);
+    if (k > 0) mass += min(ties, all) * weight(set, key_logit(key));
     const uint64_t limit = limit_of(set.top_p, mass);
-    const uint32_t at = select_key<T, true>(x, V, top, set.to_log2, table, limit, hist, sh, before);
-    const uint64_t w = weight(key_logit(at), (double)top, set.to_log2, table);
+    const uint32_t at = select_key<T, true>(x, V, set, weight, limit, hist, sh, before);
+    const uint64_t w = weight(set, key_logit(at));
     const uint64_t n = w == 0 ? (uint64_t)V : (limit - before + w - 1) / w;
     if (at > key) {
       key = at;
@@ -509,17 +585,58 @@ __device__ void slow_border(const T* x, int V, const Settings& set, int k, float
   __syncthreads();
 }
 
+// Ascending.  Up to 256: every element's place is the number of those below it, counted by four threads each.  More: a bitonic network.
+constexpr int kRanked = 256;
+__device__ __forceinline__ void sort_list(uint64_t* list, int n, uint64_t* spare, uint32_t* rank) {
+  const int tid = threadIdx.x;
+  if (n <= kRanked) {
+    const int i = tid & (kRanked - 1), part = tid / kRanked;
+    if (tid < kRanked) rank[tid] = 0;
+    __syncthreads();
+    const int each = (n + 3) / 4;
+    if (i < n) {
+      const uint64_t mine = list[i];
+      uint32_t below = 0;
+      for (int j = part * each; j < min((part + 1) * each, n); ++j) below += list[j] < mine;
+      atomicAdd(&rank[i], below);
+    }
+    __syncthreads();
+    if (tid < n) spare[rank[tid]] = list[tid];
+    __syncthreads();
+    if (tid < n) list[tid] = spare[tid];
+    __syncthreads();
+    return;
+  }
+  int n2 = 2 * kRanked;
+  while (n2 < n) n2 *= 2;
+  for (int i = n + tid; i < n2; i += kThreads) list[i] = ~0ull;
+  __syncthreads();
+  for (int size = 2; size <= n2; size *= 2)
+    for (int step = size / 2; step > 0; step /= 2) {
+      for (int i = tid; i < n2 / 2; i += kThreads) {
+        const int a = 2 * i - (i & (step - 1)), b = a + step;
+        const uint64_t xa = list[a], xb = list[b];
+        if ((xa > xb) == ((a & size) == 0)) {
+          list[a] = xb;
+          list[b] = xa;
+        }
+      }
+      __syncthreads();
+    }
+}
+__device__ __forceinline__ uint32_t listed_key(uint64_t x) { return ~(uint32_t)(x >> 32); }
+
 // grid: (rows)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
   __shared__ uint64_t list[kList];
-  __shared__ double table[kTable];
-  __shared__ uint64_t sh[kWaves];
-  __shared__ float tops[kMostSlices];
-  __shared__ double factor[kMostSlices];
-  __shared__ unsigned long long kept[kMostSlices];       // weight that a slice keeps, relative to its maximum
+  __shared__ uint64_t spare[kRanked];
+  __shared__ uint32_t rank[kRanked];
+  __shared__ double table[kBins];
+  __shared__ uint64_t sh[2 * kWaves];
+  __shared__ unsigned long long kept[kMostSlices];       // weight that a slice keeps
   __shared__ int at_slice;
-  __shared__ uint64_t in_slice, row_total;
+  __shared__ uint64_t in_slice;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x;
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const RowPlan plan = p.plan[r];
@@ -531,42 +648,23 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
     }
     return;
   }
+  if (tid < p.slices) kept[tid] = plan.how == kSlow ? 0 : p.stats[(int64_t)r * p.slices + tid].above;
+  if (plan.how == kFromList)
+    for (int i = tid; i < plan.listed; i += kThreads) list[i] = p.list[(int64_t)r * kList + i];
   const Settings set(p, r);
-  fill_table(table);
-  if (tid < p.slices) {
-    const SliceStats st = p.stats[(int64_t)r * p.slices + tid];
-    tops[tid] = st.top;
-    factor[tid] = factor_of(st.top, top, set.to_log2);
-    kept[tid] = plan.how == kEverything ? st.total : plan.how == kFromList ? st.above : 0;
-  }
+  Weights::fill(set, table);
+  const Weights weight(set, top, table);
+  __syncthreads();
   uint32_t key = 0;
   int index = p.V;
   if (plan.how == kFromList) {
     const int n = plan.listed;
-    int n2 = 64;
-    while (n2 < n) n2 *= 2;
-    for (int i = tid; i < n2; i += kThreads) list[i] = i < n ? p.list[(int64_t)r * kList + i] : ~0ull;
-    __syncthreads();
-    for (int size = 2; size <= n2; size *= 2)
-      for (int step = size / 2; step > 0; step /= 2) {
-        for (int i = tid; i < n2 / 2; i += kThreads) {
-          const int a = 2 * i - (i & (step - 1)), b = a + step;
-          const uint64_t xa = list[a], xb = list[b];
-          if ((xa > xb) == ((a & size) == 0)) {
-            list[a] = xb;
-            list[b] = xa;
-          }
-        }
-        __syncthreads();
-      }
-    const auto weight_at = [&](int i) -> uint64_t {
-      return i < n ? weight(key_logit(~(uint32_t)(list[i] >> 32)), (double)top, set.to_log2, table) : 0;
-    };
+    sort_list(list, n, spare, rank);
     const int n_k = plan.k > 0 ? min(plan.k, n) : n;
     uint64_t limit = plan.limit, all;
     if (plan.k > 0 && set.top_p < 1.f) {
       uint64_t w = 0;
-      for (int i = tid; i < n_k; i += kThreads) w += weight_at(i);
+      for (int i = tid; i < n_k; i += kThreads) w += weight(set, key_logit(listed_key(list[i])));
       block_scan64(w, sh, all);
       limit = limit_of(set.top_p, all);
     }
@@ -574,76 +672,66 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
     uint64_t before = plan.above, stay = 0;
     for (int i0 = 0; i0 < n_k; i0 += kThreads) {
       const int i = i0 + tid;
-      const uint64_t w = weight_at(i);
+      const uint32_t ki = i < n_k ? listed_key(list[i]) : 0;
+      const uint64_t w = i < n_k ? weight(set, key_logit(ki)) : 0;
       const uint64_t upto = before + block_scan64(w, sh, all);
-      stay += i < n_k && (set.top_p == 1.f || upto - w < limit) && ~(uint32_t)(list[min(i, n2 - 1)] >> 32) >= least;
+      const bool stays = i < n_k && (set.top_p == 1.f || upto - w < limit) && ki >= least;
+      stay += stays;
       before += all;
+      if (stays) atomicAdd(&kept[(int)(uint32_t)list[i] / p.slice], (unsigned long long)w);
     }
     block_scan64(stay, sh, all);
-    const int kept_n = (int)all;
-    if (kept_n > 0) {
-      key = ~(uint32_t)(list[kept_n - 1] >> 32);
-      index = (int)(uint32_t)list[kept_n - 1];
+    if (all > 0) {
+      key = listed_key(list[all - 1]);
+      index = (int)(uint32_t)list[all - 1];
     } else {
       key = least;
     }
-    for (int i = tid; i < kept_n; i += kThreads) {
-      const int s = (int)(uint32_t)list[i] / p.slice;
-      atomicAdd(&kept[s], (unsigned long long)weight(key_logit(~(uint32_t)(list[i] >> 32)), (double)tops[s], set.to_log2, table));
-    }
-  }
-  __syncthreads();
-  if (plan.how == kSlow) {
-    slow_border<T>(x, p.V, set, plan.k, top, table, reinterpret_cast<unsigned long long*>(list), sh, key, index);
+  } else if (plan.how == kSlow) {
+    slow_border<T>(x, p.V, set, plan.k, top, weight, reinterpret_cast<unsigned long long*>(list), sh, key, index);
     for (int s = 0; s < p.slices; ++s) {
-      if (tops[s] == -INFINITY) continue;
       uint64_t w = 0, all;
       for (int v = s * p.slice + tid; v < min((s + 1) * p.slice, p.V); v += kThreads) {
         const float f = clean(load1(x + v));
         const uint32_t kf = score_key(f);
-        if (kf > key || (kf == key && v <= index)) w += weight(f, (double)tops[s], set.to_log2, table);
+        if (f > -INFINITY && (kf > key || (kf == key && v <= index))) w += weight(set, f);
       }
       block_scan64(w, sh, all);
       if (tid == 0) kept[s] = all;
     }
-    __syncthreads();
   }
+  __syncthreads();
   // the target, and the slice it falls in
-  if (tid == 0) {
-    uint64_t total = 0;
-    for (int s = 0; s < p.slices; ++s) total += scaled(kept[s], factor[s]);
-    row_total = total;
+  if (wave == 0) {
+    const uint64_t a = 2 * lane < p.slices ? kept[2 * lane] : 0, b = 2 * lane + 1 < p.slices ? kept[2 * lane + 1] : 0;
+    const uint64_t upto = wave_scan64(a + b), total = lane64(upto, 63), front = upto - a - b;
     const double t = p.tokens ? (double)p.u[r] * (double)total : 0.0;
     uint64_t target = t > 0.0 ? (uint64_t)t : 0;
     target = min(target, total - 1);
-    int s = 0;
-    for (; s < p.slices - 1; ++s) {
-      const uint64_t m = scaled(kept[s], factor[s]);
-      if (target < m) break;
-      target -= m;
+    if (front <= target && target < upto) {
+      const bool second = target >= front + a;
+      at_slice = 2 * lane + (second ? 1 : 0);
+      in_slice = target - front - (second ? a : 0);
     }
-    at_slice = s;
-    in_slice = target;
-    p.border[r] = Border{key, index, 1.0 / (double)total};
+    if (lane == 0) p.border[r] = Border{key, index, 1.0 / (double)total};
   }
-  __syncthreads();
   if (!p.tokens) return;
+  __syncthreads();
   // the token: the wavefronts take consecutive shares of the slice
   const int s = at_slice, end = min((s + 1) * p.slice, p.V), share = p.slice / kWaves, v0 = s * p.slice + wave * share;
-  const float slice_top = tops[s];
-  const double f_s = factor[s];
-  const uint64_t target = in_slice;
+  const int v1 = min(v0 + share, end);
   const auto kept_weights = [&](int v, uint64_t (&w)[4]) {
     const float4 f = logits4(x, v, end);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float l = get(f, e);
       const uint32_t kf = score_key(l);
-      w[e] = l > -INFINITY && (kf > key || (kf == key && v + e <= index)) ? weight(l, (double)slice_top, set.to_log2, table) : 0;
+      w[e] = l > -INFINITY && (kf > key || (kf == key && v + e <= index)) ? weight(set, l) : 0;
     }
   };
   uint64_t sum = 0;
-  for (int v = v0 + 4 * lane; v < min(v0 + share, end); v += 256) {
+#pragma unroll 4
+  for (int v = v0 + 4 * lane; v < v1; v += 256) {
     uint64_t w[4];
     kept_weights(v, w);
     sum += (w[0] + w[1]) + (w[2] + w[3]);
@@ -651,27 +739,30 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
   sum = wave_sum64(sum);
   if (lane == 0) sh[wave] = sum;
   __syncthreads();
-  uint64_t run = 0;
-  for (int w = 0; w < wave; ++w) run += sh[w];
-  if (scaled(run, f_s) > target || !(scaled(run + sum, f_s) > target)) return;
-  for (int v = v0 + 4 * lane; v - 4 * lane < min(v0 + share, end); v += 256) {
-    uint64_t w[4];
-    kept_weights(v, w);
-    const uint64_t mine = (w[0] + w[1]) + (w[2] + w[3]), upto = run + wave_scan64(mine, lane);
-    const uint64_t hit = __ballot(scaled(upto, f_s) > target);
+  const uint64_t upto_wave = wave_scan64(lane < kWaves ? sh[lane] : 0), in_all = lane64(upto_wave, kWaves - 1);
+  // (the bins' weights, rounded once each, may add up to a little more than the tokens': then it is the slice's last)
+  const uint64_t target = in_all > 0 ? min(in_slice, in_all - 1) : 0;
+  uint64_t run = lane64(upto_wave, __builtin_amdgcn_readfirstlane(wave)) - sum;
+  if (in_all == 0 && tid == 0) p.tokens[r] = index < p.V ? index : s * p.slice;
+  if (run > target || run + sum <= target) return;
+  for (int v = v0 + 4 * lane; v - 4 * lane < v1; v += 256) {
+    uint64_t w[4] = {0, 0, 0, 0};
+    if (v < v1) kept_weights(v, w);
+    const uint64_t mine = (w[0] + w[1]) + (w[2] + w[3]), upto = run + wave_scan64(mine);
+    const uint64_t hit = __ballot(upto > target);
     if (hit) {
       if (lane == __builtin_ctzll(hit)) {
         uint64_t c = upto - mine;
         int e = 0;
         for (; e < 3; ++e) {
           c += w[e];
-          if (scaled(c, f_s) > target) break;
+          if (c > target) break;
         }
         p.tokens[r] = v + e;
       }
       return;
     }
-    run = __shfl((unsigned long long)upto, 63, 64);
+    run = lane64(upto, 63);
   }
 }
 
@@ -680,16 +771,18 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
 // grid: (slices, rows)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_probs_kernel(SampleParams p) {
-  __shared__ double table[kTable];
+  __shared__ float table[kBins];                         // a bin's weight over the total
   const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
   const Settings set(p, r);
   const Border border = p.border[r];
-  const float top = p.plan[r].top;
-  fill_table(table);
+  const float top = p.plan[r].top, first = set.bin_of(top), z = place_factor(set);
+  const double to_prob = border.inv_total * (double)(1ull << kFraction);
+  table[tid] = (float)(bin_weight((float)tid, set) * to_prob);
   __syncthreads();
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   float* const out = p.probs + (int64_t)r * p.V;
   const int end = min((s + 1) * p.slice, p.V);
+#pragma unroll 4
   for (int v = s * p.slice + 4 * tid; v < end; v += 4 * kThreads) {
     const float4 f = logits4(x, v, end);
     float4_u w;
@@ -697,8 +790,12 @@ __global__ __launch_bounds__(kThreads) void sample_probs_kernel(SampleParams p) 
     for (int e = 0; e < 4; ++e) {
       const float l = get(f, e);
       const uint32_t kf = score_key(l);
-      const bool keep = l > -INFINITY && (kf > border.key || (kf == border.key && v + e <= border.index));
-      w[e] = keep ? (float)(weight_real(l, (double)top, set.to_log2, table) * border.inv_total) : 0.f;
+      w[e] = 0.f;
+      if (l > -INFINITY && (kf > border.key || (kf == border.key && v + e <= border.index))) {
+        float place;
+        const float b = first - set.bin_of(l, place), g = b < (float)kBins ? table[(int)b] : (float)(bin_weight(b, set) * to_prob);
+        w[e] = __builtin_fmaf(g, place_excess(place, z), g);
+      }
     }
     if (v + 3 < end) {
       *reinterpret_cast<float4_u*>(out + v) = w;
@@ -722,7 +819,7 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Layout {
   int slice, slices;
-  size_t stats, mass, count, list, plan, border, bytes;
+  size_t stats, bins, list, plan, border, bytes;
   Layout(int rows, int V) {
     slice = slice_of(rows, V);
     slices = (V + slice - 1) / slice;
@@ -730,10 +827,8 @@ struct Layout {
     size_t off = 0;
     stats = off;
     off += align256(n * sizeof(SliceStats));
-    mass = off;
+    bins = off;
     off += align256(n * kBins * sizeof(uint64_t));
-    count = off;
-    off += align256(n * kBins * sizeof(uint32_t));
     list = off;
     off += align256((size_t)rows * kList * sizeof(uint64_t));
     plan = off;
@@ -800,8 +895,7 @@ int svf_sample(const void* logits, int32_t dtype, int64_t logits_stride, int32_t
   p.slice = at.slice;
   p.slices = at.slices;
   p.stats = reinterpret_cast<svf::SliceStats*>(w + at.stats);
-  p.mass = reinterpret_cast<uint64_t*>(w + at.mass);
-  p.count = reinterpret_cast<uint32_t*>(w + at.count);
+  p.bins = reinterpret_cast<uint64_t*>(w + at.bins);
   p.list = reinterpret_cast<uint64_t*>(w + at.list);
   p.plan = reinterpret_cast<svf::RowPlan*>(w + at.plan);
   p.border = reinterpret_cast<svf::Border*>(w + at.border);

@@ -1,6 +1,6 @@
 """svf_sample against the fp64 oracle.
 
-Bars.  Weights are good to 2^-30 relative, sums of them are exact, so a drawn token is right when the
+Bars.  Weights are good to 2^-27 relative, and so are their cumulative sums, so a drawn token is right when the
 target lies in its interval of the oracle's cumulative weights widened by 1e-8 of the total (it is the
 oracle's own token otherwise: counted); what a row keeps is the oracle's set, unless some token is within 1e-8 of
 the top-p border.  Probabilities: fp32, 2^-20 relative."""
