@@ -19,7 +19,7 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 512, kWaves = 8;
 constexpr int kKeys = 64;                                // keys of a unit
 constexpr int kMostB = 4096;
 constexpr float kRescaleGap = 8.0f;                      // log2 units the maximum in use may lag behind
@@ -191,7 +191,7 @@ struct Kernel {
 };
 
 template <int D, int RB>
-__global__ __launch_bounds__(kThreads, 1) void chunk_attn_kernel(ChunkParams p) {
+__global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) {
   typedef Kernel<D, RB> C;
   constexpr int R = C::R;
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -452,11 +452,11 @@ hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
 }  // namespace
 
 size_t chunk_attn_workspace(const svf_chunk_shape_t& s) {
-  return s.d == 128 ? Parts<128, Kernel<128, 2>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64, 2>::R>::bytes(kWorkgroups);
+  return s.d == 128 ? Parts<128, Kernel<128, 1>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64, 1>::R>::bytes(kWorkgroups);
 }
 
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st) {
-  return p.d == 128 ? launch_d<128, 2>(p, st) : launch_d<64, 2>(p, st);
+  return p.d == 128 ? launch_d<128, 1>(p, st) : launch_d<64, 1>(p, st);
 }
 
 }  // namespace svf
