@@ -56,6 +56,9 @@ struct Item {
 template <int R>
 __device__ __forceinline__ int items_of(const ChunkParams& p, const ChunkSeq& s) { return (s.n * p.G + R - 1) / R; }
 
+// a value that all lanes hold, in a scalar register
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 __device__ __forceinline__ ChunkSeq load_seq(const ChunkParams& p, int b) {
   return chunk_seq(p.seq_lens[b], p.new_rows[b], p.new_lens[b], p.max_seq_len, p.max_new, p.n_rows);
 }
@@ -168,15 +171,16 @@ struct Parts {
   static size_t bytes(int n) { return (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
 };
 
-template <int D, int RB>
+template <int D>
 struct Kernel {
-  static constexpr int R = kWaves * 32 * RB;             // rows of an item
+  static constexpr int R = kWaves * 32;                  // rows of an item
   static constexpr int kRowBytes = 2 * D;
   static constexpr int kChunks = D / 8;                  // sixteen-byte chunks of a row
   static constexpr int kTileBytes = kKeys * kRowBytes;   // K or V of a unit
   static constexpr int kRowsPerPass = kThreads / kChunks;
   static constexpr int kPasses = kKeys / kRowsPerPass;
-  static constexpr int kLds = 4 * kTileBytes > (kMostB + 1) * 8 ? 4 * kTileBytes : (kMostB + 1) * 8;
+  static constexpr int kLds = 8 * kTileBytes;            // four units; at first the sums over the sequences
+  static_assert((kMostB + 1) * 8 <= kLds, "");
 
   // K chunk c of key t at c ^ (t mod 16) (d = 64, two rows to a line of banks: c ^ (t / 2 mod 8)): sixteen lanes that read the same chunk of
   // sixteen keys hit all banks.
@@ -190,12 +194,12 @@ struct Kernel {
   }
 };
 
-template <int D, int RB>
+template <int D>
 __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) {
-  typedef Kernel<D, RB> C;
+  typedef Kernel<D> C;
   constexpr int R = C::R;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hh = lane >> 5, r32 = lane & 31;
+  __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), hh = lane >> 5, r32 = lane & 31;
   const int me = blockIdx.x;
   const Parts<D, R> parts(p.ws, gridDim.x);
 
@@ -205,33 +209,44 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   const int N = (int)min((int64_t)gridDim.x, total);     // workgroups with work: one unit at least
   if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
   if (me >= N) return;
-  int64_t at = total * me / N;
+  const int64_t at = total * me / N;
   const int64_t end = total * (me + 1) / N;
   Cursor c = cursor_at<R>(p, cum, at);
+  c.b = uniform(c.b);
+  c.h = uniform(c.h);
+  c.item = uniform(c.item);
+  int skip = uniform((int)c.skip), left = uniform((int)(end - at));      // units of the item in front of the range; units to do
   __syncthreads();
 
   const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
-  while (at < end) {
-    const ChunkSeq s = load_seq(p, c.b);
+  const bool second = wave >= kWaves / 2;
+  while (left > 0) {
+    ChunkSeq s = load_seq(p, c.b);
+    s = {uniform(s.len), uniform(s.row), uniform(s.n)};
     const Item<R> it(p, s, c.item);
-    const int n = (int)min((int64_t)it.units - c.skip, end - at);        // units of this item in the range
-    const int unit0 = it.unit0 + (int)c.skip;
+    const int n = min(it.units - skip, left);              // units of this item in the range
+    const int unit0 = it.unit0 + skip;
     const char* const K = static_cast<const char*>(p.K) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
     const char* const V = static_cast<const char*>(p.V) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
 
-    const auto place = [&](int unit, int i) -> int64_t {                 // bytes from the pool's start
-      const int t = min(max(unit * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last);
-      if (p.kv.page_size == 0) return 2 * ((int64_t)c.b * p.kv.stride_page + (int64_t)t * p.kv.stride_tok);
-      const int np = p.kv.page_shift >= 0 ? t >> p.kv.page_shift : t / p.kv.page_size;
-      int page = p.table[(int64_t)c.b * p.kv.max_pages + np];
-      if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
-      return 2 * ((int64_t)page * p.kv.stride_page + (int64_t)(t - np * p.kv.page_size) * p.kv.stride_tok);
-    };
+    // A thread's chunks of a unit: looked up in the page table two units ahead of their request, requested one unit ahead of their way
+    // into LDS.  Places outside what the item's rows see are read as the nearest one inside.
+    const int32_t* const table = p.table + (int64_t)c.b * p.kv.max_pages;
+    int page[C::kPasses];
     u32x4 kx[C::kPasses], vx[C::kPasses];
-    const auto request = [&](int unit) {
+    const auto token = [&](int u, int i) { return min(max((unit0 + u) * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last); };
+    const auto page_of = [&](int t) { return p.kv.page_shift >= 0 ? t >> p.kv.page_shift : t / p.kv.page_size; };
+    const auto look_up = [&](int u) {
+#pragma unroll
+      for (int i = 0; i < C::kPasses; ++i) page[i] = p.kv.page_size == 0 ? c.b : table[page_of(token(u, i))];
+    };
+    const auto request = [&](int u) {
 #pragma unroll
       for (int i = 0; i < C::kPasses; ++i) {
-        const int64_t off = place(unit, i);
+        int slot = token(u, i);
+        if (p.kv.page_size != 0) slot -= page_of(slot) * p.kv.page_size;
+        const int pg = (uint32_t)page[i] < (uint32_t)p.n_pages ? page[i] : 0;
+        const int64_t off = 2 * ((int64_t)pg * p.kv.stride_page + (int64_t)slot * p.kv.stride_tok);
         kx[i] = *reinterpret_cast<const u32x4*>(K + off);
         vx[i] = *reinterpret_cast<const u32x4*>(V + off);
       }
@@ -246,141 +261,161 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
         *reinterpret_cast<u32x4*>(v + C::v_at(t, c_lane)) = vx[i];
       }
     };
-    request(unit0);
+    look_up(0);
+    request(0);
+    if (n > 1) look_up(1);
 
-    // this lane's rows: r32 of each of the wavefront's RB blocks
-    bf16x8 qf[RB][D / 16];
-    int hi[RB], lo[RB];
-    floatx16 o[RB][D / 32] = {};
-    float m[RB], l[RB];
-    const bool rows_here = wave * 32 * RB < it.rows;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = it.row0 + min(wave * 32 * RB + 32 * rb + r32, it.rows - 1), j = r / p.G;
+    // this lane's row
+    bf16x8 qf[D / 16];
+    floatx16 o[D / 32] = {};
+    const int row = it.row0 + min(wave * 32 + r32, it.rows - 1), row_j = row / p.G;
+    const int hi = s.len + row_j, lo = p.window > 0 ? hi + 1 - p.window : 0;
+    {
       const char* qr = static_cast<const char*>(p.q) +
-                       2 * ((int64_t)(s.row + j) * p.q_stride + (int64_t)(c.h * p.G + r - j * p.G) * D) + 16 * hh;
+                       2 * ((int64_t)(s.row + row_j) * p.q_stride + (int64_t)(c.h * p.G + row - row_j * p.G) * D) + 16 * hh;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) qf[rb][ks] = *reinterpret_cast<const bf16x8*>(qr + 32 * ks);
-      hi[rb] = s.len + j;
-      lo[rb] = p.window > 0 ? hi[rb] + 1 - p.window : 0;
-      m[rb] = -INFINITY;
-      l[rb] = 0.f;
+      for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qr + 32 * ks);
     }
+    float m = -INFINITY, l = 0.f;
     // units whose keys every row of the item sees need no mask
     const int hi_all = s.len + it.row0 / p.G, lo_all = p.window > 0 ? it.last + 1 - p.window : 0;
 
+    floatx16 sc[2];
+    bf16x8 pf[4];
+    // K Q^T of a unit
+    const auto scores = [&](int buf) {
+      const char* const k = lds + buf * 2 * C::kTileBytes;
+      sc[0] = sc[1] = floatx16{};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
+          sc[kk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], sc[kk], 0, 0, 0);
+        }
+    };
+    // V^T P^T of a unit.  V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels 16 (g mod 2) + 4 x .. + 3 of key j
+    // of the four keys of its half, and receives channel lane mod 16 of those keys
+    const int vt = 4 * hh + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vb = 8 * (lane & 1);
+    const auto outputs = [&](int buf) {
+      const char* const v = lds + buf * 2 * C::kTileBytes + C::kTileBytes;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) {
+          shortx4 x[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
+          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[kb], o[cb], 0, 0, 0);
+        }
+    };
+    // the unit's scores into weights.  The maximum in use may lag behind by kRescaleGap: most units leave it as it is
+    const auto weights = [&](int u) {
+      const int key0 = (unit0 + u) * kKeys;
+      if (key0 + kKeys - 1 > hi_all || key0 < lo_all) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
+            if (key > hi || key < lo) sc[kk][i] = -INFINITY;
+          }
+      }
+      float use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kk][i] = __builtin_fmaf(sc[kk][i], p.scale_log2, -use);
+      float top = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
+      top = halves_max(top);
+      // (a row whose keys so far are all masked keeps -inf and weights of zero)
+      if (__ballot(top > kRescaleGap || (m == -INFINITY && top > -INFINITY))) {
+        const float up = m == -INFINITY ? (top > -INFINITY ? top : 0.f) : fmaxf(top, 0.f);
+        const float f = __builtin_amdgcn_exp2f(-up);
+        if (m > -INFINITY || top > -INFINITY) m = use + up;
+        l *= f;
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[kk][i] -= up;
+      }
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int b8 = 0; b8 < 2; ++b8) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = __builtin_amdgcn_exp2f(sc[kk][8 * b8 + 2 * i]), y = __builtin_amdgcn_exp2f(sc[kk][8 * b8 + 2 * i + 1]);
+            l += x + y;
+            w[i] = pack_bf16(x, y);
+          }
+          pf[2 * kk + b8] = __builtin_bit_cast(bf16x8, w);
+        }
+    };
     put(0);
-    if (n > 1) request(unit0 + 1);
+    if (n > 1) {
+      request(1);
+      if (n > 2) look_up(2);
+      put(1);
+      if (n > 2) {
+        request(2);
+        if (n > 3) look_up(3);
+      }
+    }
+    __syncthreads();
+    // The first four wavefronts and the second four, one of each on a SIMD, are a phase apart: while the ones multiply (the outputs of a unit
+    // and the scores of the next) the others work out weights and bring a unit into LDS.  A unit's place among the four is free when
+    // both have multiplied by its values, and the unit after next is put there.
+    if (second) __syncthreads();
+    scores(0);
     __syncthreads();
     for (int u = 0; u < n; ++u) {
-      const int key0 = (unit0 + u) * kKeys;
-      if (u + 1 < n) {
-        put((u + 1) & 1);
-        if (u + 2 < n) request(unit0 + u + 2);
-      }
-      if (rows_here) {
-        const char* const k = lds + (u & 1) * 2 * C::kTileBytes;
-        const char* const v = k + C::kTileBytes;
-        floatx16 sc[2][RB] = {};
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              sc[kk][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[rb][ks], sc[kk][rb], 0, 0, 0);
-          }
-        if (key0 + kKeys - 1 > hi_all || key0 < lo_all) {
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
-                if (key > hi[rb] || key < lo[rb]) sc[kk][rb][i] = -INFINITY;
-              }
+      if (u + 2 < n) {
+        put((u + 2) & 3);
+        if (u + 3 < n) {
+          request(u + 3);
+          if (u + 4 < n) look_up(u + 4);
         }
-        bf16x8 pf[RB][4];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          float top = fmaxf(sc[0][rb][0], sc[1][rb][0]);
-#pragma unroll
-          for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[0][rb][i], sc[1][rb][i]));
-          top = halves_max(top) * p.scale_log2;
-          // (a row whose keys so far are all masked keeps -inf and weights of zero)
-          if (__ballot(top > m[rb] + kRescaleGap || (m[rb] == -INFINITY && top > m[rb]))) {
-            const float now = fmaxf(m[rb], top);
-            const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[rb] - now);
-            m[rb] = now;
-            l[rb] *= f;
-#pragma unroll
-            for (int cb = 0; cb < D / 32; ++cb) o[rb][cb] *= f;
-          }
-          const float use = m[rb] == -INFINITY ? 0.f : m[rb];
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-            for (int b8 = 0; b8 < 2; ++b8) {
-              u32x4 w;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kk][rb][8 * b8 + 2 * i], p.scale_log2, -use));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kk][rb][8 * b8 + 2 * i + 1], p.scale_log2, -use));
-                l[rb] += x + y;
-                w[i] = pack_bf16(x, y);
-              }
-              pf[rb][2 * kk + b8] = __builtin_bit_cast(bf16x8, w);
-            }
-        }
-        // V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels 16 (g mod 2) + 4 x .. + 3 of key j of the
-        // four keys of its half, and receives channel lane mod 16 of those keys
-        const int vt = 4 * hh + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vb = 8 * (lane & 1);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-          for (int cb = 0; cb < D / 32; ++cb) {
-            shortx4 x[2];
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-              x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
-            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              o[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[rb][kb], o[rb][cb], 0, 0, 0);
-          }
       }
+      weights(u);
+      __syncthreads();
+      outputs(u & 3);
+      scores((u + 1) & 3);                                 // (of nothing behind the last unit)
       __syncthreads();
     }
+    if (!second) __syncthreads();
 
     // this item's result, whole or a part
-    const bool begins = c.skip == 0, ends = c.skip + n == it.units;
+    const bool begins = skip == 0, ends = skip + n == it.units;
     const int slot = begins ? 1 : 0;
     if (begins && !ends && tid == 0) {
-      const int64_t last_unit = at + it.units - 1;
+      const int64_t last_unit = end - left + it.units - 1;
       parts.join[me] = make_int4(c.b, c.h, c.item, (int)(((last_unit + 1) * N - 1) / total));
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = wave * 32 * RB + 32 * rb + r32;
-      const float den = halves_sum(l[rb]);
-      if (r >= it.rows) continue;
+    const int r = wave * 32 + r32;
+    const float den = halves_sum(l);
+    if (r < it.rows) {
       if (begins && ends) {
-        const int row = it.row0 + r, j = row / p.G, head = c.h * p.G + row - j * p.G;
+        const int head = c.h * p.G + row - row_j * p.G;
         const float inv = 1.0f / den;
-        char* to = static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D) + 8 * hh;
+        char* to = static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + row_j) * p.out_stride + (int64_t)head * D) + 8 * hh;
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const u32x2 w = {pack_bf16(o[rb][cb][4 * g] * inv, o[rb][cb][4 * g + 1] * inv),
-                             pack_bf16(o[rb][cb][4 * g + 2] * inv, o[rb][cb][4 * g + 3] * inv)};
+            const u32x2 w = {pack_bf16(o[cb][4 * g] * inv, o[cb][4 * g + 1] * inv),
+                             pack_bf16(o[cb][4 * g + 2] * inv, o[cb][4 * g + 3] * inv)};
             *reinterpret_cast<u32x2*>(to + 64 * cb + 16 * g) = w;
           }
-        if (p.lse && hh == 0)
-          p.lse[(int64_t)(s.row + j) * p.Hq + head] = (m[rb] + log2f(den)) * 0.69314718055994530942f;
+        if (p.lse && hh == 0) p.lse[(int64_t)(s.row + row_j) * p.Hq + head] = (m + log2f(den)) * 0.69314718055994530942f;
       } else {
         const int64_t at_part = (int64_t)(2 * me + slot) * R + r;
         float* to = parts.o + at_part * D + 4 * hh;
@@ -388,22 +423,22 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
         for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const floatx4 x = {o[rb][cb][4 * g], o[rb][cb][4 * g + 1], o[rb][cb][4 * g + 2], o[rb][cb][4 * g + 3]};
+            const floatx4 x = {o[cb][4 * g], o[cb][4 * g + 1], o[cb][4 * g + 2], o[cb][4 * g + 3]};
             *reinterpret_cast<floatx4*>(to + 32 * cb + 8 * g) = x;
           }
-        if (hh == 0) parts.ml[at_part] = make_float2(m[rb], den);
+        if (hh == 0) parts.ml[at_part] = make_float2(m, den);
       }
     }
 
     // the next item
-    at += n;
-    c.skip = 0;
+    left -= n;
+    skip = 0;
     if (++c.item == items_of<R>(p, s)) {
       c.item = 0;
       if (++c.h == p.Hkv) {
         c.h = 0;
         ++c.b;
-        while (at < end && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with units: at < end)
+        while (left > 0 && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with units: some are left)
       }
     }
   }
@@ -441,10 +476,10 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
 
 constexpr int kWorkgroups = 256;
 
-template <int D, int RB>
+template <int D>
 hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
-  typedef Kernel<D, RB> C;
-  hipLaunchKernelGGL((chunk_attn_kernel<D, RB>), dim3(kWorkgroups), dim3(kThreads), C::kLds, st, p);
+  typedef Kernel<D> C;
+  hipLaunchKernelGGL(chunk_attn_kernel<D>, dim3(kWorkgroups), dim3(kThreads), 0, st, p);
   hipLaunchKernelGGL((chunk_merge_kernel<D, C::R>), dim3(kWorkgroups), dim3(kThreads), 0, st, p);
   return hipGetLastError();
 }
@@ -452,11 +487,11 @@ hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
 }  // namespace
 
 size_t chunk_attn_workspace(const svf_chunk_shape_t& s) {
-  return s.d == 128 ? Parts<128, Kernel<128, 1>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64, 1>::R>::bytes(kWorkgroups);
+  return s.d == 128 ? Parts<128, Kernel<128>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64>::R>::bytes(kWorkgroups);
 }
 
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st) {
-  return p.d == 128 ? launch_d<128, 1>(p, st) : launch_d<64, 1>(p, st);
+  return p.d == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
 }
 
 }  // namespace svf
