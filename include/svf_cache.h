@@ -53,7 +53,7 @@ typedef struct svf_chunk_shape {
   int32_t max_new;           /* new tokens a sequence may have in one call, >= 1              */
   int32_t n_rows;            /* rows of q, k_new, v_new and the outputs, >= 1                 */
   int32_t window;            /* a token sees the last `window` tokens, itself included; 0: all */
-  int64_t kv_stride_page, kv_stride_tok, kv_stride_head; /* as in svf_shape_t                 */
+  int64_t kv_stride_page, kv_stride_tok, kv_stride_head; /* as in svf_shape_t, below 2^34 elements */
   int64_t q_stride, k_stride, v_stride, out_stride;      /* elements between rows; 0: dense   */
   float sm_scale;            /* softmax scale; <= 0 selects 1/sqrt(d)                         */
   int32_t rotary_dim;        /* leading channels that are rotated: 0 (none) or a multiple of 16, <= d */

@@ -22,6 +22,7 @@ typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
 constexpr int kThreads = 512, kWaves = 8;
 constexpr int kKeys = 64;                                // keys of a unit
 constexpr int kMostB = 4096;
+constexpr int kXcds = 8;
 constexpr float kRescaleGap = 8.0f;                      // log2 units the maximum in use may lag behind
 
 __device__ __forceinline__ float halves_sum(float x) {
@@ -200,13 +201,14 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   constexpr int R = C::R;
   __shared__ __attribute__((aligned(16))) char lds[C::kLds];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), hh = lane >> 5, r32 = lane & 31;
-  const int me = blockIdx.x;
   const Parts<D, R> parts(p.ws, gridDim.x);
 
   int64_t* const cum = reinterpret_cast<int64_t*>(lds);
   units_before<R>(p, cum);
   const int64_t total = cum[p.B];
   const int N = (int)min((int64_t)gridDim.x, total);     // workgroups with work: one unit at least
+  // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
+  const int me = N == (int)gridDim.x ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
   if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
   if (me >= N) return;
   const int64_t at = total * me / N;
@@ -232,23 +234,24 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     // A thread's chunks of a unit: looked up in the page table two units ahead of their request, requested one unit ahead of their way
     // into LDS.  Places outside what the item's rows see are read as the nearest one inside.
     const int32_t* const table = p.table + (int64_t)c.b * p.kv.max_pages;
-    int page[C::kPasses];
+    uint32_t page[C::kPasses], slot[C::kPasses];
     u32x4 kx[C::kPasses], vx[C::kPasses];
-    const auto token = [&](int u, int i) { return min(max((unit0 + u) * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last); };
-    const auto page_of = [&](int t) { return p.kv.page_shift >= 0 ? t >> p.kv.page_shift : t / p.kv.page_size; };
     const auto look_up = [&](int u) {
 #pragma unroll
-      for (int i = 0; i < C::kPasses; ++i) page[i] = p.kv.page_size == 0 ? c.b : table[page_of(token(u, i))];
+      for (int i = 0; i < C::kPasses; ++i) {
+        const uint32_t t = (uint32_t)min(max((unit0 + u) * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last);
+        const uint32_t np = p.page.of(t);
+        slot[i] = t - np * (uint32_t)p.kv.page_size;
+        page[i] = p.kv.page_size == 0 ? (uint32_t)c.b : (uint32_t)table[np];
+      }
     };
     const auto request = [&](int u) {
 #pragma unroll
       for (int i = 0; i < C::kPasses; ++i) {
-        int slot = token(u, i);
-        if (p.kv.page_size != 0) slot -= page_of(slot) * p.kv.page_size;
-        const int pg = (uint32_t)page[i] < (uint32_t)p.n_pages ? page[i] : 0;
-        const int64_t off = 2 * ((int64_t)pg * p.kv.stride_page + (int64_t)slot * p.kv.stride_tok);
-        kx[i] = *reinterpret_cast<const u32x4*>(K + off);
-        vx[i] = *reinterpret_cast<const u32x4*>(V + off);
+        const uint32_t pg = page[i] < (uint32_t)p.n_pages ? page[i] : 0;
+        const uint64_t off = (uint64_t)slot[i] * p.tok16 + (uint64_t)pg * p.page16;
+        kx[i] = *reinterpret_cast<const u32x4*>(K + 16 * off);
+        vx[i] = *reinterpret_cast<const u32x4*>(V + 16 * off);
       }
     };
     const auto put = [&](int buf) {
@@ -282,35 +285,82 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
 
     floatx16 sc[2];
     bf16x8 pf[4];
-    // K Q^T of a unit
-    const auto scores = [&](int buf) {
-      const char* const k = lds + buf * 2 * C::kTileBytes;
-      sc[0] = sc[1] = floatx16{};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const bf16x8 a = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
-          sc[kk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[ks], sc[kk], 0, 0, 0);
-        }
-    };
-    // V^T P^T of a unit.  V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels 16 (g mod 2) + 4 x .. + 3 of key j
-    // of the four keys of its half, and receives channel lane mod 16 of those keys
+    // The two products of a unit, K Q^T (scores) and V^T P^T (outputs), four instructions at a time: operands() reads the four's K or V
+    // fragments out of LDS, multiply() takes them.  V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels
+    // 16 (g mod 2) + 4 x .. + 3 of key j of the four keys of its half, and receives channel lane mod 16 of those keys.
+    constexpr int kGroups = D / 32;
     const int vt = 4 * hh + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vb = 8 * (lane & 1);
-    const auto outputs = [&](int buf) {
+    const auto k_operands = [&](int buf, int g, bf16x8 (&a)[4]) {
+      const char* const k = lds + buf * 2 * C::kTileBytes;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ks = 2 * g + i / 2, kk = i & 1;
+        a[i] = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
+      }
+    };
+    const auto k_multiply = [&](int g, const bf16x8 (&a)[4]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ks = 2 * g + i / 2, kk = i & 1;
+        sc[kk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[ks], ks == 0 ? floatx16{} : sc[kk], 0, 0, 0);
+      }
+    };
+    const auto v_operands = [&](int buf, int g, bf16x8 (&a)[4]) {
       const char* const v = lds + buf * 2 * C::kTileBytes + C::kTileBytes;
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
+      for (int i = 0; i < 4; ++i) {
+        const int kb = (4 * g + i) / (D / 32), cb = (4 * g + i) % (D / 32);
+        shortx4 x[2];
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) {
-          shortx4 x[2];
+        for (int y = 0; y < 2; ++y)
+          x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
+        a[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    };
+    const auto v_multiply = [&](int g, const bf16x8 (&a)[4]) {
 #pragma unroll
-          for (int y = 0; y < 2; ++y)
-            x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
-          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-          o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[kb], o[cb], 0, 0, 0);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const int kb = (4 * g + i) / (D / 32), cb = (4 * g + i) % (D / 32);
+        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], pf[kb], o[cb], 0, 0, 0);
+      }
+    };
+    // A multiplying phase.  Operands are read four products ahead of the ones that take them (the scheduler, left alone, puts every read right
+    // in front of its product and waits a trip to LDS for each); the first four's are in `x` already.
+    bf16x8 x[4], y[4];
+#define SVF_IN_ORDER() __builtin_amdgcn_sched_barrier(0x6)
+    const auto scores_after = [&](int buf) {             // (x: the first K operands)
+#pragma unroll
+      for (int g = 0; g < kGroups; g += 2) {
+        k_operands(buf, g + 1, y);
+        SVF_IN_ORDER();
+        k_multiply(g, x);
+        SVF_IN_ORDER();
+        if (g + 2 < kGroups) k_operands(buf, g + 2, x);
+        SVF_IN_ORDER();
+        k_multiply(g + 1, y);
+        SVF_IN_ORDER();
+      }
+    };
+    const auto outputs_then_scores = [&](int u) {
+#pragma unroll
+      for (int g = 0; g < kGroups; g += 2) {
+        v_operands(u & 3, g + 1, y);
+        SVF_IN_ORDER();
+        v_multiply(g, x);
+        SVF_IN_ORDER();
+        if (g + 2 < kGroups) v_operands(u & 3, g + 2, x);
+        else k_operands((u + 1) & 3, 0, x);
+        SVF_IN_ORDER();
+        v_multiply(g + 1, y);
+        SVF_IN_ORDER();
+      }
+      scores_after((u + 1) & 3);
+    };
+    const auto phase_ends = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
     };
     // the unit's scores into weights.  The maximum in use may lag behind by kRescaleGap: most units leave it as it is
     const auto weights = [&](int u) {
@@ -375,8 +425,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     // and the scores of the next) the others work out weights and bring a unit into LDS.  A unit's place among the four is free when
     // both have multiplied by its values, and the unit after next is put there.
     if (second) __syncthreads();
-    scores(0);
-    __syncthreads();
+    k_operands(0, 0, x);
+    scores_after(0);
+    phase_ends();
     for (int u = 0; u < n; ++u) {
       if (u + 2 < n) {
         put((u + 2) & 3);
@@ -386,16 +437,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
         }
       }
       weights(u);
-      __syncthreads();
-      outputs(u & 3);
-      scores((u + 1) & 3);                                 // (of nothing behind the last unit)
-      __syncthreads();
+      v_operands(u & 3, 0, x);
+      phase_ends();
+      outputs_then_scores(u);                              // (scores of nothing behind the last unit)
+      phase_ends();
     }
     if (!second) __syncthreads();
 
     // this item's result, whole or a part
     const bool begins = skip == 0, ends = skip + n == it.units;
-    const int slot = begins ? 1 : 0;
+    const int part = begins ? 1 : 0;
     if (begins && !ends && tid == 0) {
       const int64_t last_unit = end - left + it.units - 1;
       parts.join[me] = make_int4(c.b, c.h, c.item, (int)(((last_unit + 1) * N - 1) / total));
@@ -417,7 +468,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
           }
         if (p.lse && hh == 0) p.lse[(int64_t)(s.row + row_j) * p.Hq + head] = (m + log2f(den)) * 0.69314718055994530942f;
       } else {
-        const int64_t at_part = (int64_t)(2 * me + slot) * R + r;
+        const int64_t at_part = (int64_t)(2 * me + part) * R + r;
         float* to = parts.o + at_part * D + 4 * hh;
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)

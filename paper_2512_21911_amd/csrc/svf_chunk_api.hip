@@ -22,6 +22,8 @@ int check_chunk_shape(const svf_chunk_shape_t* s) {
   const int vec = s->dtype == SVF_F32 ? 4 : 8;
   if (s->kv_stride_tok < s->d || s->kv_stride_head < s->d || s->kv_stride_page < s->d) return SVF_ERR_SHAPE;
   if (s->kv_stride_tok % vec || s->kv_stride_head % vec || s->kv_stride_page % vec) return SVF_ERR_SHAPE;
+  // (strides in sixteen-byte chunks are 32-bit numbers too)
+  if ((s->kv_stride_tok | s->kv_stride_head | s->kv_stride_page) >> 34) return SVF_ERR_SHAPE;
   const int64_t q_row = (int64_t)s->Hq * s->d, kv_row = (int64_t)s->Hkv * s->d;
   if (or_dense(s->q_stride, q_row) < q_row || or_dense(s->out_stride, q_row) < q_row ||
       or_dense(s->k_stride, kv_row) < kv_row || or_dense(s->v_stride, kv_row) < kv_row) return SVF_ERR_SHAPE;
@@ -121,6 +123,9 @@ int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K,
   if (!ws || misaligned(ws, kAlign) || ws_bytes < workspace_of(*shape)) return SVF_ERR_WORKSPACE;
   svf::ChunkParams p;
   p.kv = layout_of(*shape);
+  p.page = svf::PageOf(shape->page_size);
+  p.page16 = (uint32_t)(shape->kv_stride_page / 8);
+  p.tok16 = (uint32_t)(shape->kv_stride_tok / 8);
   p.q = q;
   p.K = K;
   p.V = V;

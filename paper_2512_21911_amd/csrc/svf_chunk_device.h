@@ -6,8 +6,22 @@
 
 namespace svf {
 
+// The page of a place, t < 2^30, without a division: 4 t m / 2^(32 + s) with m = ceil(2^(30 + s) / page_size), 2^s >= page_size.  What m
+// is too large by, less than one, adds less than t / 2^(30 + s) <= 1 / page_size: never a whole page.  (m has at most 32 bits.)
+struct PageOf {
+  uint32_t m, s;
+  __host__ explicit PageOf(int page_size) : m(0), s(0) {
+    if (page_size <= 0) return;                          // contiguous: page 0 of the sequence's own
+    while ((1ll << s) < page_size) ++s;
+    m = (uint32_t)(((1ull << (30 + s)) + (uint64_t)page_size - 1) / (uint64_t)page_size);
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t t) const { return __umulhi(4 * t, m) >> s; }
+};
+
 struct ChunkParams {
   KvLayout kv;
+  PageOf page{0};
+  uint32_t page16, tok16;    // strides of the cache in sixteen-byte chunks (bf16)
   const void* q;
   const void* K;
   const void* V;
