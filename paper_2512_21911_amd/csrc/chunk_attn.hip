@@ -23,7 +23,6 @@ constexpr int kThreads = 512, kWaves = 8;
 constexpr int kKeys = 64;                                // keys of a unit
 constexpr int kMostB = 4096;
 constexpr int kXcds = 8;
-constexpr float kRescaleGap = 8.0f;                      // log2 units the maximum in use may lag behind
 
 __device__ __forceinline__ float halves_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -362,40 +361,18 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
     };
-    // the unit's scores into weights.  The maximum in use may lag behind by kRescaleGap: most units leave it as it is
-    const auto weights = [&](int u) {
-      const int key0 = (unit0 + u) * kKeys;
-      if (key0 + kKeys - 1 > hi_all || key0 < lo_all) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
-            if (key > hi || key < lo) sc[kk][i] = -INFINITY;
-          }
-      }
-      float use = m == -INFINITY ? 0.f : m;
+    // A unit's scores into weights, 2^(score - m), and their sum into l.  m need not be the maximum: weights, sums and outputs are
+    // floating point, and good as long as nothing overflows.  So the maximum of the first unit that a row sees serves until a unit's weights
+    // sum to more than 2^40 in some row (the sums are there anyway; looking for the maximum of every unit cost a tenth of the time),
+    // and then the unit is done again with the maximum it has.  Units that need masks look for theirs.
+    const auto exponents = [&](float use) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[kk][i] = __builtin_fmaf(sc[kk][i], p.scale_log2, -use);
-      float top = fmaxf(sc[0][0], sc[1][0]);
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
-      top = halves_max(top);
-      // (a row whose keys so far are all masked keeps -inf and weights of zero)
-      if (__ballot(top > kRescaleGap || (m == -INFINITY && top > -INFINITY))) {
-        const float up = m == -INFINITY ? (top > -INFINITY ? top : 0.f) : fmaxf(top, 0.f);
-        const float f = __builtin_amdgcn_exp2f(-up);
-        if (m > -INFINITY || top > -INFINITY) m = use + up;
-        l *= f;
-#pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sc[kk][i] -= up;
-      }
+    };
+    const auto exponentials = [&]() {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -404,11 +381,58 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float x = __builtin_amdgcn_exp2f(sc[kk][8 * b8 + 2 * i]), y = __builtin_amdgcn_exp2f(sc[kk][8 * b8 + 2 * i + 1]);
-            l += x + y;
+            sum[i & 1] += x;
+            sum[2 + (i & 1)] += y;
             w[i] = pack_bf16(x, y);
           }
           pf[2 * kk + b8] = __builtin_bit_cast(bf16x8, w);
         }
+      return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    // (sc: exponents relative to m, or to 0 for a row that has seen nothing)
+    const auto rebase = [&]() {
+      float top = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
+      top = halves_max(top);
+      float up = 0.f;                                      // (a row whose keys so far are all masked keeps -inf and weights of zero)
+      if (top > -INFINITY) {
+        up = m == -INFINITY ? top : fmaxf(top, 0.f);
+        m = (m == -INFINITY ? 0.f : m) + up;
+      }
+      const float f = __builtin_amdgcn_exp2f(-up);
+      l *= f;
+#pragma unroll
+      for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kk][i] -= up;
+    };
+    bool unseen = true;                                    // some row has seen nothing yet
+    const auto weights = [&](int u) {
+      const int key0 = (unit0 + u) * kKeys;
+      const bool masked = key0 + kKeys - 1 > hi_all || key0 < lo_all;
+      if (masked) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
+            if (key > hi || key < lo) sc[kk][i] = -INFINITY;
+          }
+      }
+      exponents(m == -INFINITY ? 0.f : m);
+      if (masked || unseen) {
+        rebase();
+        unseen = __ballot(m == -INFINITY) != 0;
+      }
+      float sum = exponentials();
+      if (__ballot(sum > 0x1p40f)) {
+        rebase();
+        sum = exponentials();
+      }
+      l += sum;
     };
     put(0);
     if (n > 1) {
