@@ -230,42 +230,52 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     const char* const K = static_cast<const char*>(p.K) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
     const char* const V = static_cast<const char*>(p.V) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
 
-    // A thread's chunks of a unit: looked up in the page table two units ahead of their request, requested one unit ahead of their way
+    // A thread's chunks of a unit: looked up in the page table one unit ahead of their request, requested one unit ahead of their way
     // into LDS.  Places outside what the item's rows see are read as the nearest one inside.
     const int32_t* const table = p.table + (int64_t)c.b * p.kv.max_pages;
-    uint32_t page[C::kPasses], slot[C::kPasses];
-    u32x4 kx[C::kPasses], vx[C::kPasses];
-    const auto look_up = [&](int u) {
+    struct Places { uint32_t page[C::kPasses], slot[C::kPasses]; };
+    struct Chunks { u32x4 k[C::kPasses], v[C::kPasses]; };
+    const auto look_up = [&](int u, Places& at) {
 #pragma unroll
       for (int i = 0; i < C::kPasses; ++i) {
         const uint32_t t = (uint32_t)min(max((unit0 + u) * kKeys + t_lane + i * C::kRowsPerPass, it.first), it.last);
         const uint32_t np = p.page.of(t);
-        slot[i] = t - np * (uint32_t)p.kv.page_size;
-        page[i] = p.kv.page_size == 0 ? (uint32_t)c.b : (uint32_t)table[np];
+        at.slot[i] = t - np * (uint32_t)p.kv.page_size;
+        at.page[i] = p.kv.page_size == 0 ? (uint32_t)c.b : (uint32_t)table[np];
       }
     };
-    const auto request = [&](int u) {
+    const auto request = [&](const Places& at, Chunks& x) {
 #pragma unroll
       for (int i = 0; i < C::kPasses; ++i) {
-        const uint32_t pg = page[i] < (uint32_t)p.n_pages ? page[i] : 0;
-        const uint64_t off = (uint64_t)slot[i] * p.tok16 + (uint64_t)pg * p.page16;
-        kx[i] = *reinterpret_cast<const u32x4*>(K + 16 * off);
-        vx[i] = *reinterpret_cast<const u32x4*>(V + 16 * off);
+        const uint32_t pg = at.page[i] < (uint32_t)p.n_pages ? at.page[i] : 0;
+        const uint64_t off = (uint64_t)at.slot[i] * p.tok16 + (uint64_t)pg * p.page16;
+        x.k[i] = *reinterpret_cast<const u32x4*>(K + 16 * off);
+        x.v[i] = *reinterpret_cast<const u32x4*>(V + 16 * off);
       }
     };
-    const auto put = [&](int buf) {
+    const auto put = [&](int buf, const Chunks& x) {
       char* const k = lds + buf * 2 * C::kTileBytes;
       char* const v = k + C::kTileBytes;
 #pragma unroll
       for (int i = 0; i < C::kPasses; ++i) {
         const int t = t_lane + i * C::kRowsPerPass;
-        *reinterpret_cast<u32x4*>(k + C::k_at(t, c_lane)) = kx[i];
-        *reinterpret_cast<u32x4*>(v + C::v_at(t, c_lane)) = vx[i];
+        *reinterpret_cast<u32x4*>(k + C::k_at(t, c_lane)) = x.k[i];
+        *reinterpret_cast<u32x4*>(v + C::v_at(t, c_lane)) = x.v[i];
       }
     };
-    look_up(0);
-    request(0);
-    if (n > 1) look_up(1);
+    Places at;
+    Chunks on_way;
+    Chunks begin[2];
+    {
+      Places a[3];
+      look_up(0, a[0]);
+      if (n > 1) look_up(1, a[1]);
+      if (n > 2) look_up(2, a[2]);
+      if (n > 3) look_up(3, at);
+      request(a[0], begin[0]);
+      if (n > 1) request(a[1], begin[1]);
+      if (n > 2) request(a[2], on_way);
+    }
 
     // this lane's row
     bf16x8 qf[D / 16];
@@ -348,6 +358,15 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
         SVF_IN_ORDER();
         v_multiply(g, x);
         SVF_IN_ORDER();
+        if (g == 0 && u + 3 < n) {
+          // Loading, in the products' shadow: unit u + 3 into LDS (both have multiplied by the values of unit u - 1, which were there), u + 4
+          // on its way, u + 5 looked up
+          put((u + 3) & 3, on_way);
+          if (u + 4 < n) {
+            request(at, on_way);
+            if (u + 5 < n) look_up(u + 5, at);
+          }
+        }
         if (g + 2 < kGroups) v_operands(u & 3, g + 2, x);
         else k_operands((u + 1) & 3, 0, x);
         SVF_IN_ORDER();
@@ -434,36 +453,27 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       }
       l += sum;
     };
-    put(0);
-    if (n > 1) {
-      request(1);
-      if (n > 2) look_up(2);
-      put(1);
-      if (n > 2) {
-        request(2);
-        if (n > 3) look_up(3);
-      }
+    put(0, begin[0]);
+    if (n > 1) put(1, begin[1]);
+    if (n > 2) put(2, on_way);
+    if (n > 3) {
+      request(at, on_way);
+      if (n > 4) look_up(4, at);
     }
     __syncthreads();
     // The first four wavefronts and the second four, one of each on a SIMD, are a phase apart: while the ones multiply (the outputs of a unit
-    // and the scores of the next) the others work out weights and bring a unit into LDS.  A unit's place among the four is free when
-    // both have multiplied by its values, and the unit after next is put there.
+    // and the scores of the next) the others work out weights.
     if (second) __syncthreads();
     k_operands(0, 0, x);
     scores_after(0);
     phase_ends();
     for (int u = 0; u < n; ++u) {
-      if (u + 2 < n) {
-        put((u + 2) & 3);
-        if (u + 3 < n) {
-          request(u + 3);
-          if (u + 4 < n) look_up(u + 4);
-        }
-      }
       weights(u);
       v_operands(u & 3, 0, x);
       phase_ends();
+      __builtin_amdgcn_s_setprio(2);                       // (the matrix cores first: 3 %)
       outputs_then_scores(u);                              // (scores of nothing behind the last unit)
+      __builtin_amdgcn_s_setprio(0);
       phase_ends();
     }
     if (!second) __syncthreads();
