@@ -49,9 +49,9 @@ typedef struct svf_chunk_shape {
   int32_t page_size;         /* tokens per physical page; 0 = contiguous cache                */
   int32_t max_pages_per_seq; /* row length of block_table (unused when page_size == 0)        */
   int32_t n_pages;           /* pages of the pool (contiguous: sequences it has room for, >= B)   */
-  int32_t max_seq_len;       /* tokens a sequence may have, the new ones included             */
-  int32_t max_new;           /* new tokens a sequence may have in one call, >= 1              */
-  int32_t n_rows;            /* rows of q, k_new, v_new and the outputs, >= 1                 */
+  int32_t max_seq_len;       /* tokens a sequence may have, the new ones included, 1..2^30    */
+  int32_t max_new;           /* new tokens a sequence may have in one call, 1..2^22          */
+  int32_t n_rows;            /* rows of q, k_new, v_new and the outputs, 1..2^28              */
   int32_t window;            /* a token sees the last `window` tokens, itself included; 0: all */
   int64_t kv_stride_page, kv_stride_tok, kv_stride_head; /* as in svf_shape_t, below 2^34 elements */
   int64_t q_stride, k_stride, v_stride, out_stride;      /* elements between rows; 0: dense   */

@@ -1,175 +1,13 @@
 // Attention of new tokens over the cache in bf16 (svf_chunk_attn).
-#include <hip/hip_bf16.h>
-#include <hip/hip_runtime.h>
-
 #include <algorithm>
 
-#include "svf_chunk_device.h"
+#include "chunk_share.h"
 
 namespace svf {
 
 namespace {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
-typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-typedef __attribute__((__vector_size__(4 * sizeof(short)))) short shortx4;
-typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
-typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
-typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
-typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
-
-constexpr int kThreads = 512, kWaves = 8;
 constexpr int kKeys = 64;                                // keys of a unit
-constexpr int kMostB = 4096;
-constexpr int kXcds = 8;
-
-__device__ __forceinline__ float halves_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float halves_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const floatx2 f = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
-}
-
-// One item: R query rows (row r = query head r % G of new token r / G) of a (sequence, KV head) against the
-// 64-key units they see.
-template <int R>
-struct Item {
-  int row0, rows, first, last, unit0, units;
-  __device__ __forceinline__ Item(const ChunkParams& p, const ChunkSeq& s, int i) {
-    const int M = s.n * p.G;
-    row0 = i * R;
-    rows = min(R, M - row0);
-    const int j0 = row0 / p.G, j1 = (row0 + rows - 1) / p.G;
-    first = p.window > 0 ? max(0, s.len + j0 + 1 - p.window) : 0;
-    last = s.len + j1;
-    unit0 = first / kKeys;
-    units = last / kKeys + 1 - unit0;
-  }
-};
-template <int R>
-__device__ __forceinline__ int items_of(const ChunkParams& p, const ChunkSeq& s) { return (s.n * p.G + R - 1) / R; }
-
-// a value that all lanes hold, in a scalar register
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ __forceinline__ ChunkSeq load_seq(const ChunkParams& p, int b) {
-  return chunk_seq(p.seq_lens[b], p.new_rows[b], p.new_lens[b], p.max_seq_len, p.max_new, p.n_rows);
-}
-
-__device__ __forceinline__ int64_t shfl_up64(int64_t x, int d) {
-  const int lo = __shfl_up((int)(x & 0xffffffff), d, 64), hi = __shfl_up((int)(x >> 32), d, 64);
-  return ((int64_t)hi << 32) | (uint32_t)lo;
-}
-__device__ __forceinline__ int64_t lane64(int64_t x, int l) {
-  const int lo = __builtin_amdgcn_readlane((int)(x & 0xffffffff), l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
-  return ((int64_t)hi << 32) | (uint32_t)lo;
-}
-__device__ __forceinline__ int64_t wave_scan64(int64_t x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = shfl_up64(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
-
-// Units of all items of one KV head of a sequence, by a wavefront.
-template <int R>
-__device__ int64_t units_of_seq(const ChunkParams& p, const ChunkSeq& s, int lane) {
-  const int n = items_of<R>(p, s);
-  int64_t sum = 0;
-  for (int i = lane; i < n; i += 64) sum += Item<R>(p, s, i).units;
-  return lane64(wave_scan64(sum, lane), 63);
-}
-
-// How the work of a call is shared: all units of all items in a row (sequence, KV head, item, unit), cut into as many
-// equal ranges as there are workgroups.
-struct Cursor {
-  int b, h, item;            // where a range begins
-  int64_t skip;              // units of that item in front of it
-  int64_t total;
-};
-// cum: [kMostB + 1] in LDS
-template <int R>
-__device__ void units_before(const ChunkParams& p, int64_t* cum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = threadIdx.x; b < p.B; b += kThreads) {
-    const ChunkSeq s = load_seq(p, b);
-    const int n = items_of<R>(p, s);
-    cum[b + 1] = n == 0 ? 0 : n == 1 ? Item<R>(p, s, 0).units : -1;
-  }
-  __syncthreads();
-  for (int b = wave; b < p.B; b += kWaves) {
-    if (cum[b + 1] >= 0) continue;
-    const int64_t u = units_of_seq<R>(p, load_seq(p, b), lane);
-    if (lane == 0) cum[b + 1] = u;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    int64_t run = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-      const int64_t x = wave_scan64(b0 + lane < p.B ? cum[b0 + lane + 1] * p.Hkv : 0, lane);
-      if (b0 + lane < p.B) cum[b0 + lane + 1] = run + x;
-      run += lane64(x, 63);
-    }
-    if (lane == 0) cum[0] = 0;
-  }
-  __syncthreads();
-}
-template <int R>
-__device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at) {
-  const int lane = threadIdx.x & 63;
-  Cursor c;
-  int lo = 0, hi = p.B - 1;                              // the last sequence with cum[b] <= at that has units
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (cum[mid] <= at) lo = mid;
-    else hi = mid - 1;
-  }
-  c.b = lo;
-  const int64_t of_seq = (cum[lo + 1] - cum[lo]) / p.Hkv;
-  int64_t rest = at - cum[lo];
-  c.h = (int)(rest / of_seq);
-  rest -= c.h * of_seq;
-  const ChunkSeq s = load_seq(p, c.b);
-  const int n = items_of<R>(p, s);
-  c.item = 0;
-  for (int i0 = 0;; i0 += 64) {
-    const int64_t x = wave_scan64(i0 + lane < n ? Item<R>(p, s, i0 + lane).units : 0, lane);
-    const uint64_t in = __ballot(rest < x);
-    if (in) {
-      const int l = __builtin_ctzll(in);
-      c.item = i0 + l;
-      if (l > 0) rest -= lane64(x, l - 1);
-      break;
-    }
-    rest -= lane64(x, 63);
-  }
-  c.skip = rest;
-  return c;
-}
-
-// The workspace: for every workgroup two partial results of R rows (0: of the item its range begins inside of, 1: of the one
-// its range ends inside of) and what the second launch joins.
-template <int D, int R>
-struct Parts {
-  float* o;                  // [N][2][R][D], relative to the maximum
-  float2* ml;                // [N][2][R] maximum (log2 units), denominator
-  int4* join;                // [N] of the item that begins in a range and ends behind it: b, KV head, item, last workgroup; b < 0: none
-  __host__ __device__ Parts(char* ws, int n) {
-    o = reinterpret_cast<float*>(ws);
-    ml = reinterpret_cast<float2*>(ws + (size_t)n * 2 * R * D * sizeof(float));
-    join = reinterpret_cast<int4*>(ws + (size_t)n * 2 * R * (D * sizeof(float) + sizeof(float2)));
-  }
-  static size_t bytes(int n) { return (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
-};
 
 template <int D>
 struct Kernel {
@@ -203,7 +41,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   const Parts<D, R> parts(p.ws, gridDim.x);
 
   int64_t* const cum = reinterpret_cast<int64_t*>(lds);
-  units_before<R>(p, cum);
+  units_before<R, kKeys>(p, cum);
   const int64_t total = cum[p.B];
   const int N = (int)min((int64_t)gridDim.x, total);     // workgroups with work: one unit at least
   // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
@@ -212,7 +50,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   if (me >= N) return;
   const int64_t at = total * me / N;
   const int64_t end = total * (me + 1) / N;
-  Cursor c = cursor_at<R>(p, cum, at);
+  Cursor c = cursor_at<R, kKeys>(p, cum, at);
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   c.item = uniform(c.item);
@@ -224,7 +62,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   while (left > 0) {
     ChunkSeq s = load_seq(p, c.b);
     s = {uniform(s.len), uniform(s.row), uniform(s.n)};
-    const Item<R> it(p, s, c.item);
+    const Item<R, kKeys> it(p, s, c.item);
     const int n = min(it.units - skip, left);              // units of this item in the range
     const int unit0 = it.unit0 + skip;
     const char* const K = static_cast<const char*>(p.K) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
@@ -529,43 +367,12 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   }
 }
 
-// Joins the parts of the items that were cut; workgroup v: the item that begins in range v.
-template <int D, int R>
-__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
-  const int N = gridDim.x, me = blockIdx.x;
-  const Parts<D, R> parts(p.ws, N);
-  const int4 join = parts.join[me];
-  if (join.x < 0) return;
-  const ChunkSeq s = load_seq(p, join.x);
-  const Item<R> it(p, s, join.z);
-  for (int i = threadIdx.x; i < it.rows * (D / 4); i += kThreads) {
-    const int r = i / (D / 4), ch = 4 * (i % (D / 4));
-    float top = parts.ml[(int64_t)(2 * me + 1) * R + r].x;
-    for (int v = me + 1; v <= join.w; ++v) top = fmaxf(top, parts.ml[(int64_t)(2 * v) * R + r].x);
-    float den = 0.f;
-    floatx4 x = {};
-    for (int v = me; v <= join.w; ++v) {
-      const int64_t at = (int64_t)(2 * v + (v == me ? 1 : 0)) * R + r;
-      const float2 ml = parts.ml[at];
-      const float f = __builtin_amdgcn_exp2f(ml.x - top);
-      den += f * ml.y;
-      x += f * *reinterpret_cast<const floatx4*>(parts.o + at * D + ch);
-    }
-    const int row = it.row0 + r, j = row / p.G, head = join.y * p.G + row - j * p.G;
-    const float inv = 1.0f / den;
-    const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
-    *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch)) = w;
-    if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
-  }
-}
-
-constexpr int kWorkgroups = 256;
-
 template <int D>
 hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
   typedef Kernel<D> C;
   hipLaunchKernelGGL(chunk_attn_kernel<D>, dim3(kWorkgroups), dim3(kThreads), 0, st, p);
-  hipLaunchKernelGGL((chunk_merge_kernel<D, C::R>), dim3(kWorkgroups), dim3(kThreads), 0, st, p);
+  hipLaunchKernelGGL((chunk_merge_kernel<D, C::R, kKeys>), dim3(kWorkgroups, (unsigned)std::min<int64_t>(C::R / 32, ((int64_t)p.max_new * p.G + 31) / 32)),
+                     dim3(kThreads), 0, st, p);
   return hipGetLastError();
 }
 

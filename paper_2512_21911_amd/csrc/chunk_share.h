@@ -1,0 +1,255 @@
+// The matrix-core kernels of svf_chunk_attn: how their work is shared out, and how what was cut is joined.
+#pragma once
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_runtime.h>
+
+#include "svf_chunk_device.h"
+
+namespace svf {
+
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short shortx4;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+
+constexpr int kThreads = 512, kWaves = 8;
+constexpr int kMostB = 4096;
+constexpr int kXcds = 8;
+
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const floatx2 f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+
+// One item: R query rows (row r = query head r % G of new token r / G) of a (sequence, KV head) against the
+// units of KEYS keys that they see.
+template <int R, int KEYS>
+struct Item {
+  int row0, rows, first, last, unit0, units;
+  __device__ __forceinline__ Item(const ChunkParams& p, const ChunkSeq& s, int i) {
+    const int M = s.n * p.G;
+    row0 = i * R;
+    rows = min(R, M - row0);
+    const int j0 = row0 / p.G, j1 = (row0 + rows - 1) / p.G;
+    first = p.window > 0 ? max(0, s.len + j0 + 1 - p.window) : 0;
+    last = s.len + j1;
+    unit0 = first / KEYS;
+    units = last / KEYS + 1 - unit0;
+  }
+};
+template <int R>
+__device__ __forceinline__ int items_of(const ChunkParams& p, const ChunkSeq& s) { return (s.n * p.G + R - 1) / R; }
+
+// a value that all lanes hold, in a scalar register
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ ChunkSeq load_seq(const ChunkParams& p, int b) {
+  return chunk_seq(p.seq_lens[b], p.new_rows[b], p.new_lens[b], p.max_seq_len, p.max_new, p.n_rows);
+}
+
+__device__ __forceinline__ int64_t shfl_up64(int64_t x, int d) {
+  const int lo = __shfl_up((int)(x & 0xffffffff), d, 64), hi = __shfl_up((int)(x >> 32), d, 64);
+  return ((int64_t)hi << 32) | (uint32_t)lo;
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int l) {
+  const int lo = __builtin_amdgcn_readlane((int)(x & 0xffffffff), l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
+  return ((int64_t)hi << 32) | (uint32_t)lo;
+}
+__device__ __forceinline__ int64_t wave_scan64(int64_t x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t y = shfl_up64(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Units of all items of one KV head of a sequence, by a wavefront.
+template <int R, int KEYS>
+__device__ int64_t units_of_seq(const ChunkParams& p, const ChunkSeq& s, int lane) {
+  const int n = items_of<R>(p, s);
+  int64_t sum = 0;
+  for (int i = lane; i < n; i += 64) sum += Item<R, KEYS>(p, s, i).units;
+  return lane64(wave_scan64(sum, lane), 63);
+}
+
+// How the work of a call is shared: all units of all items in a row (sequence, KV head, item, unit), cut into as many
+// equal ranges as there are workgroups.
+struct Cursor {
+  int b, h, item;            // where a range begins
+  int64_t skip;              // units of that item in front of it
+  int64_t total;
+};
+// cum: [kMostB + 1] in LDS
+template <int R, int KEYS>
+__device__ void units_before(const ChunkParams& p, int64_t* cum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = threadIdx.x; b < p.B; b += kThreads) {
+    const ChunkSeq s = load_seq(p, b);
+    const int n = items_of<R>(p, s);
+    cum[b + 1] = n == 0 ? 0 : n == 1 ? Item<R, KEYS>(p, s, 0).units : -1;
+  }
+  __syncthreads();
+  for (int b = wave; b < p.B; b += kWaves) {
+    if (cum[b + 1] >= 0) continue;
+    const int64_t u = units_of_seq<R, KEYS>(p, load_seq(p, b), lane);
+    if (lane == 0) cum[b + 1] = u;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    int64_t run = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+      const int64_t x = wave_scan64(b0 + lane < p.B ? cum[b0 + lane + 1] * p.Hkv : 0, lane);
+      if (b0 + lane < p.B) cum[b0 + lane + 1] = run + x;
+      run += lane64(x, 63);
+    }
+    if (lane == 0) cum[0] = 0;
+  }
+  __syncthreads();
+}
+template <int R, int KEYS>
+__device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at) {
+  const int lane = threadIdx.x & 63;
+  Cursor c;
+  int lo = 0, hi = p.B - 1;                              // the last sequence with cum[b] <= at that has units
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (cum[mid] <= at) lo = mid;
+    else hi = mid - 1;
+  }
+  c.b = lo;
+  const int64_t of_seq = (cum[lo + 1] - cum[lo]) / p.Hkv;
+  int64_t rest = at - cum[lo];
+  c.h = (int)(rest / of_seq);
+  rest -= c.h * of_seq;
+  const ChunkSeq s = load_seq(p, c.b);
+  const int n = items_of<R>(p, s);
+  c.item = 0;
+  for (int i0 = 0;; i0 += 64) {
+    const int64_t x = wave_scan64(i0 + lane < n ? Item<R, KEYS>(p, s, i0 + lane).units : 0, lane);
+    const uint64_t in = __ballot(rest < x);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      c.item = i0 + l;
+      if (l > 0) rest -= lane64(x, l - 1);
+      break;
+    }
+    rest -= lane64(x, 63);
+  }
+  c.skip = rest;
+  return c;
+}
+
+// The workspace: for every workgroup two partial results of R rows (0: of the item its range begins inside of, 1: of the one
+// its range ends inside of) and what the second launch joins.
+template <int D, int R>
+struct Parts {
+  float* o;                  // [N][2][R][D], relative to the maximum
+  float2* ml;                // [N][2][R] maximum (log2 units), denominator
+  int4* join;                // [N] of the item that begins in a range and ends behind it: b, KV head, item, last workgroup; b < 0: none
+  __host__ __device__ Parts(char* ws, int n) {
+    o = reinterpret_cast<float*>(ws);
+    ml = reinterpret_cast<float2*>(ws + (size_t)n * 2 * R * D * sizeof(float));
+    join = reinterpret_cast<int4*>(ws + (size_t)n * 2 * R * (D * sizeof(float) + sizeof(float2)));
+  }
+  static size_t bytes(int n) { return (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
+};
+
+// Joins the parts of the items that were cut: workgroup (v, y) rows 32 y .. 32 y + 31 of the item that begins in range v.  A thread adds up four
+// channels of a row; where rows are few, several threads take the parts in turn.
+template <int D, int R, int KEYS>
+__global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
+  __shared__ floatx4 others[kThreads];
+  __shared__ float2 others_ml[kThreads];
+  const int N = gridDim.x, me = blockIdx.x, tid = threadIdx.x;
+  const Parts<D, R> parts(p.ws, N);
+  const int4 join = parts.join[me];
+  if (join.x < 0) return;
+  const ChunkSeq s = load_seq(p, join.x);
+  const Item<R, KEYS> it(p, s, join.z);
+  const int r0 = 32 * blockIdx.y, rows = min(32, it.rows - r0);
+  if (rows <= 0) return;
+  const int cells = rows * (D / 4);
+  int takers = 1;                                         // threads of a cell
+  while (2 * takers * cells <= kThreads && takers < 16) takers *= 2;
+  const int n = join.w - me + 1;
+  for (int c0 = 0; c0 < cells; c0 += kThreads / takers) {
+    const int cell = c0 + tid / takers, first = tid % takers;
+    const bool live = cell < cells;
+    const int r = r0 + (live ? cell : 0) / (D / 4), ch = 4 * (cell % (D / 4));
+    float top = -INFINITY, den = 0.f;
+    floatx4 x = {};
+    for (int i0 = first; i0 < n; i0 += 4 * takers) {
+      float2 ml[4];
+      floatx4 y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = min(i0 + k * takers, n - 1);
+        const int64_t at = (int64_t)(2 * (me + i) + (i == 0 ? 1 : 0)) * R + r;
+        ml[k] = parts.ml[at];
+        y[k] = *reinterpret_cast<const floatx4*>(parts.o + at * D + ch);
+      }
+      float now = top;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k * takers >= n) ml[k].x = -INFINITY;
+        now = fmaxf(now, ml[k].x);
+      }
+      const float use = now == -INFINITY ? 0.f : now, f0 = __builtin_amdgcn_exp2f(top - use);
+      den *= f0;
+      x *= f0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k].x - use);
+        if (i0 + k * takers < n) {
+          den += f * ml[k].y;
+          x += f * y[k];
+        }
+      }
+      top = now;
+    }
+    if (takers > 1) {
+      __syncthreads();
+      others[tid] = x;
+      others_ml[tid] = make_float2(top, den);
+      __syncthreads();
+      if (first == 0) {
+        for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k].x);
+        den = 0.f;
+        x = floatx4{};
+        for (int k = 0; k < takers; ++k) {
+          const float f = __builtin_amdgcn_exp2f(others_ml[tid + k].x - top);
+          den += f * others_ml[tid + k].y;
+          x += f * others[tid + k];
+        }
+      }
+    }
+    if (!live || first != 0) continue;
+    const int row = it.row0 + r, j = row / p.G, head = join.y * p.G + row - j * p.G;
+    const float inv = 1.0f / den;
+    const u32x2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+    *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch)) = w;
+    if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
+  }
+}
+
+constexpr int kWorkgroups = 256;                         // one on each compute unit
+
+}  // namespace
+
+}  // namespace svf

@@ -18,7 +18,7 @@ int check_chunk_shape(const svf_chunk_shape_t* s) {
   if (s->page_size < 0 || s->n_pages < 1 || s->max_seq_len < 1 || s->max_new < 1 || s->n_rows < 1 || s->window < 0)
     return SVF_ERR_SHAPE;
   // (places in a sequence, and places plus a tile, are 32-bit numbers)
-  if (s->max_seq_len > (1 << 30) || s->max_new > (1 << 24) || s->n_rows > (1 << 28)) return SVF_ERR_SHAPE;
+  if (s->max_seq_len > (1 << 30) || s->max_new > (1 << 22) || s->n_rows > (1 << 28)) return SVF_ERR_SHAPE;
   const int vec = s->dtype == SVF_F32 ? 4 : 8;
   if (s->kv_stride_tok < s->d || s->kv_stride_head < s->d || s->kv_stride_page < s->d) return SVF_ERR_SHAPE;
   if (s->kv_stride_tok % vec || s->kv_stride_head % vec || s->kv_stride_page % vec) return SVF_ERR_SHAPE;
