@@ -379,10 +379,12 @@ hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
 }  // namespace
 
 size_t chunk_attn_workspace(const svf_chunk_shape_t& s) {
+  if (chunk_attn_is_few(s.Hq / s.Hkv, s.max_new)) return chunk_attn_few_workspace(s.d);
   return s.d == 128 ? Parts<128, Kernel<128>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64>::R>::bytes(kWorkgroups);
 }
 
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st) {
+  if (chunk_attn_is_few(p.G, p.max_new)) return launch_chunk_attn_few(p, st);
   return p.d == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
 }
 

@@ -70,6 +70,10 @@ __device__ __forceinline__ ChunkSeq chunk_seq(int len, int row, int n, int max_s
 hipError_t launch_append_kv(const AppendParams& p, int dtype, hipStream_t st);
 size_t chunk_attn_workspace(const svf_chunk_shape_t& s);
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st);
+// few rows per (sequence, KV head): a kernel of its own
+bool chunk_attn_is_few(int G, int max_new);
+size_t chunk_attn_few_workspace(int d);
+hipError_t launch_chunk_attn_few(const ChunkParams& p, hipStream_t st);
 size_t chunk_attn_f32_workspace(const svf_chunk_shape_t& s);
 hipError_t launch_chunk_attn_f32(const ChunkParams& p, hipStream_t st);
 
