@@ -81,7 +81,9 @@ int svf_append_kv(const svf_chunk_shape_t* shape, const void* k_new, const void*
 
 /*
  * Bytes of device workspace svf_chunk_attn needs for `shape` (a multiple of 256; 0 if the shape is
- * invalid).  It needs no initialisation; calls that share one must be ordered on one stream.
+ * invalid).  As svf_workspace_bytes' (svf.h): 256-byte aligned, cleared to zero once (svf_workspace_init) before
+ * its first use, left reusable by every call; calls that share one must be ordered on one stream.
+ * Unlike that one's it serves every shape that needs no more bytes.
  */
 size_t svf_chunk_workspace_bytes(const svf_chunk_shape_t* shape);
 

@@ -396,10 +396,13 @@ def svf_chunk_workspace_bytes(shape: SvfChunkShape) -> int:
 
 
 def new_chunk_workspace(shape: SvfChunkShape, device="cuda") -> torch.Tensor:
+    """Allocate (through torch) and clear a workspace for `shape`."""
     n = svf_chunk_workspace_bytes(shape)
     if n == 0:
         raise SvfError(-2, "svf_chunk_workspace_bytes")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    svf_workspace_init(ws)
+    return ws
 
 
 def svf_sample_workspace_bytes(rows: int, V: int) -> int:

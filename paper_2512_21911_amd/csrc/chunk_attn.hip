@@ -48,8 +48,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   const int me = N == (int)gridDim.x ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
   if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
   if (me >= N) return;
-  const int64_t at = total * me / N;
-  const int64_t end = total * (me + 1) / N;
+  const int64_t at = range_begin(total, N, me), end = range_begin(total, N, me + 1);
   Cursor c = cursor_at<R, kKeys>(p, cum, at);
   c.b = uniform(c.b);
   c.h = uniform(c.h);
@@ -321,7 +320,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     const int part = begins ? 1 : 0;
     if (begins && !ends && tid == 0) {
       const int64_t last_unit = end - left + it.units - 1;
-      parts.join[me] = make_int4(c.b, c.h, c.item, (int)(((last_unit + 1) * N - 1) / total));
+      parts.join[me] = make_int4(c.b, c.h, c.item, owner_of(total, N, last_unit));
     }
     const int r = wave * 32 + r32;
     const float den = halves_sum(l);

@@ -214,8 +214,8 @@ template <int D>
 void launch_d(const ChunkParams& p, hipStream_t st) {
   const int n_splits = splits_of(p.B, p.Hkv, p.G, p.max_new, p.max_seq_len, p.window);
   const int64_t tiles = row_tiles(p.max_new, p.G), groups = (int64_t)p.B * p.Hkv * tiles, items = groups * n_splits;
-  float* part_o = reinterpret_cast<float*>(p.ws);
-  float2* part_ml = reinterpret_cast<float2*>(p.ws + (n_splits > 1 ? items * kRows * D * sizeof(float) : 0));
+  float* part_o = reinterpret_cast<float*>(p.ws + kChunkCounters);
+  float2* part_ml = reinterpret_cast<float2*>(p.ws + kChunkCounters + (n_splits > 1 ? items * kRows * D * sizeof(float) : 0));
   hipLaunchKernelGGL(chunk_attn_f32_kernel<D>, dim3((unsigned)std::min<int64_t>(items, 1 << 20)), dim3(kThreads), 0, st, p,
                      n_splits, tiles, items, part_o, part_ml);
   if (n_splits > 1)
@@ -227,8 +227,8 @@ void launch_d(const ChunkParams& p, hipStream_t st) {
 
 size_t chunk_attn_f32_workspace(const svf_chunk_shape_t& s) {
   const int G = s.Hq / s.Hkv, n = splits_of(s.B, s.Hkv, G, s.max_new, s.max_seq_len, s.window);
-  if (n == 1) return 256;
-  return (size_t)((int64_t)s.B * s.Hkv * row_tiles(s.max_new, G) * n) * kRows * (s.d * sizeof(float) + sizeof(float2));
+  if (n == 1) return kChunkCounters;
+  return kChunkCounters + (size_t)((int64_t)s.B * s.Hkv * row_tiles(s.max_new, G) * n) * kRows * (s.d * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_chunk_attn_f32(const ChunkParams& p, hipStream_t st) {

@@ -39,23 +39,50 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
   static_assert(kOwn == kFewRows * D * 4, "");
   __shared__ __attribute__((aligned(16))) char lds[kWaves * kOwn];
   __shared__ float2 joint[kWaves][kFewRows];
+  __shared__ bool joins;
   static_assert((kMostB + 1) * 8 <= kWaves * kOwn, "");
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), hh = lane >> 5, r32 = lane & 31;
   const Parts<D, R> parts(p.ws, gridDim.x);
 
-  int64_t* const cum = reinterpret_cast<int64_t*>(lds);
-  units_before<R, kFewKeys>(p, cum);
-  const int64_t total = cum[p.B];
-  const int N = (int)min((int64_t)gridDim.x, total);
-  const int me = N == (int)gridDim.x ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
-  if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
-  if (me >= N) return;
-  const int64_t at = total * me / N, end = total * (me + 1) / N;
-  Cursor c = cursor_at<R, kFewKeys>(p, cum, at);
+  // where this workgroup's range begins
+  int64_t total, at, end;
+  Cursor c;
+  int N, me;
+  const auto place = [&]() {
+    N = (int)min((int64_t)kWorkgroups, total);
+    me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+    at = range_begin(total, N, me);
+    end = range_begin(total, N, me + 1);
+  };
+  if (p.B <= 64 && p.unit_bound < (1 << 30)) {
+    // up to 64 sequences: lane b has sequence b, every wavefront for itself
+    const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
+    const int units = lane < p.B && s.n > 0 ? Item<R, kFewKeys>(p, s, 0).units : 0;
+    int upto = units * p.Hkv;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(upto, d, 64);
+      if (lane >= d) upto += y;
+    }
+    total = __builtin_amdgcn_readlane(upto, 63);
+    place();
+    if (me >= N) return;
+    c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
+    const int of_seq = __builtin_amdgcn_readlane(units, c.b), rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - of_seq * p.Hkv);
+    c.h = (int)((uint32_t)rest / (uint32_t)of_seq);
+    c.skip = rest - c.h * of_seq;
+  } else {
+    int64_t* const cum = reinterpret_cast<int64_t*>(lds);
+    units_before<R, kFewKeys>(p, cum);
+    total = cum[p.B];
+    place();
+    if (me >= N) return;
+    c = cursor_at<R, kFewKeys>(p, cum, at);
+    __syncthreads();
+  }
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   int skip = uniform((int)c.skip), left = uniform((int)(end - at));
-  __syncthreads();
 
   char* const mine = lds + wave * kOwn;
   const int c_lane = lane % C::kChunks, t_lane = lane / C::kChunks;
@@ -190,13 +217,18 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
       if (hh == 0) joint[wave][r32] = make_float2(m, l);
     }
     __syncthreads();
-    const bool begins = skip == 0, ends = skip + n == it.units;
-    const int part = begins ? 1 : 0;
-    if (begins && !ends && tid == 0) {
-      const int64_t last_unit = end - left + it.units - 1;
-      parts.join[me] = make_int4(c.b, c.h, 0, (int)(((last_unit + 1) * N - 1) / total));
-    }
-    for (int i = tid; i < it.rows * (D / 4); i += kThreads) {
+    const bool whole = skip == 0 && n == it.units;
+    const int64_t first_unit = end - left - skip;           // of the item
+    const int from = whole ? me : owner_of(total, N, first_unit), upto = whole ? me : owner_of(total, N, first_unit + it.units - 1);
+    const auto write = [&](int r, int ch, float top, float den, floatx4 y) {
+      const int j = r / p.G, head = c.h * p.G + r - j * p.G;
+      const float inv = 1.0f / den;
+      const u32x2 w = {pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
+      *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch)) = w;
+      if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
+    };
+    const int cells = it.rows * (D / 4);
+    for (int i = tid; i < cells; i += kThreads) {
       const int r = i / (D / 4), ch = 4 * (i % (D / 4));
       float top = joint[0][r].x;
 #pragma unroll
@@ -211,16 +243,82 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
         den += f * ml.y;
         y += f * *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(lds + w * kOwn) + r * D + ch);
       }
-      if (begins && ends) {
-        const int j = r / p.G, head = c.h * p.G + r - j * p.G;
-        const float inv = 1.0f / den;
-        const u32x2 w = {pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
-        *reinterpret_cast<u32x2*>(static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch)) = w;
-        if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
+      if (whole) {
+        write(r, ch, top, den, y);
       } else {
-        const int64_t at_part = (int64_t)(2 * me + part) * R + r;
-        *reinterpret_cast<floatx4*>(parts.o + at_part * D + ch) = y;
-        if (ch == 0) parts.ml[at_part] = make_float2(top, den);
+        const int64_t at_part = (int64_t)(2 * me + (me == from ? 1 : 0)) * R + r;
+        store_shared(parts.o + at_part * D + ch, y);
+        if (ch == 0) store_shared(&parts.ml[at_part], make_float2(top, den));
+      }
+    }
+    if (!whole) {
+      // The workgroup that comes last joins the parts, in their order: the sum does not depend on which one it is
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): this thread's stores are where the others read
+      __syncthreads();
+      if (tid == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(&parts.arrived[from], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        joins = before == (uint32_t)(upto - from);
+        if (joins) __hip_atomic_store(&parts.arrived[from], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (joins) {
+        int takers = 1;                                     // threads of a cell
+        while (2 * takers * cells <= kThreads && takers < 16) takers *= 2;
+        floatx4* const others = reinterpret_cast<floatx4*>(lds);
+        float2* const others_ml = reinterpret_cast<float2*>(lds + kThreads * sizeof(floatx4));
+        const int parts_n = upto - from + 1;
+        for (int c0 = 0; c0 < cells; c0 += kThreads / takers) {
+          const int cell = c0 + tid / takers, first = tid % takers;
+          const int r = (cell < cells ? cell : 0) / (D / 4), ch = 4 * (cell % (D / 4));
+          float top = -INFINITY, den = 0.f;
+          floatx4 y = {};
+          for (int i0 = first; i0 < parts_n; i0 += 4 * takers) {
+            float2 ml[4];
+            floatx4 z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int i = min(i0 + k * takers, parts_n - 1);
+              const int64_t at_part = (int64_t)(2 * (from + i) + (i == 0 ? 1 : 0)) * R + r;
+              ml[k] = load_shared(&parts.ml[at_part]);
+              z[k] = load_shared(parts.o + at_part * D + ch);
+            }
+            float now = top;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (i0 + k * takers >= parts_n) ml[k].x = -INFINITY;
+              now = fmaxf(now, ml[k].x);
+            }
+            const float use = now == -INFINITY ? 0.f : now, f0 = __builtin_amdgcn_exp2f(top - use);
+            den *= f0;
+            y *= f0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (i0 + k * takers < parts_n) {
+                const float f = __builtin_amdgcn_exp2f(ml[k].x - use);
+                den += f * ml[k].y;
+                y += f * z[k];
+              }
+            top = now;
+          }
+          if (takers > 1) {
+            others[tid] = y;
+            others_ml[tid] = make_float2(top, den);
+            __syncthreads();
+            if (first == 0) {
+              for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k].x);
+              den = 0.f;
+              y = floatx4{};
+              for (int k = 0; k < takers; ++k) {
+                const float f = __builtin_amdgcn_exp2f(others_ml[tid + k].x - top);
+                den += f * others_ml[tid + k].y;
+                y += f * others[tid + k];
+              }
+            }
+            __syncthreads();
+          }
+          if (cell < cells && first == 0) write(r, ch, top, den, y);
+        }
       }
     }
     __syncthreads();
@@ -238,7 +336,6 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
 template <int D>
 hipError_t launch_few_d(const ChunkParams& p, hipStream_t st) {
   hipLaunchKernelGGL(chunk_attn_few_kernel<D>, dim3(kWorkgroups), dim3(kThreads), 0, st, p);
-  hipLaunchKernelGGL((chunk_merge_kernel<D, kFewRows, kFewKeys>), dim3(kWorkgroups), dim3(kThreads), 0, st, p);
   return hipGetLastError();
 }
 

@@ -155,6 +155,42 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
   return c;
 }
 
+constexpr int kWorkgroups = 256;                         // one on each compute unit
+
+// Loads and stores of what workgroups on different XCDs exchange: at the scope of the device, past the L2s.
+__device__ __forceinline__ void store_shared(float* p, floatx4 x) {
+  const u32x4 w = __builtin_bit_cast(u32x4, x);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)w[1] << 32 | w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p) + 1, (uint64_t)w[3] << 32 | w[2], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void store_shared(float2* p, float2 x) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(x.y) << 32 | __float_as_uint(x.x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t load_shared64(const void* p) {
+  return __hip_atomic_load(static_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ floatx4 load_shared(const float* p) {
+  const uint64_t a = load_shared64(p), b = load_shared64(p + 2);
+  const u32x4 w = {(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+  return __builtin_bit_cast(floatx4, w);
+}
+__device__ __forceinline__ float2 load_shared(const float2* p) {
+  const uint64_t a = load_shared64(p);
+  return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
+}
+
+// Workgroup v of n takes units [range_begin(v), range_begin(v + 1)); n is kWorkgroups, or the number of units if that is less.
+__device__ __forceinline__ int64_t range_begin(int64_t total, int n, int v) {
+  return n == kWorkgroups ? (total * v) / kWorkgroups : (int64_t)v;
+}
+__device__ __forceinline__ int owner_of(int64_t total, int n, int64_t unit) {
+  if (n != kWorkgroups) return (int)unit;
+  // the largest v with total v / n <= unit, rounded down
+  if (total < (1 << 22)) return (int)((uint32_t)((unit + 1) * kWorkgroups - 1) / (uint32_t)total);
+  return (int)(((unit + 1) * kWorkgroups - 1) / total);
+}
+
 // The workspace: for every workgroup two partial results of R rows (0: of the item its range begins inside of, 1: of the one
 // its range ends inside of) and what the second launch joins.
 template <int D, int R>
@@ -162,12 +198,16 @@ struct Parts {
   float* o;                  // [N][2][R][D], relative to the maximum
   float2* ml;                // [N][2][R] maximum (log2 units), denominator
   int4* join;                // [N] of the item that begins in a range and ends behind it: b, KV head, item, last workgroup; b < 0: none
+  uint32_t* arrived;         // [N] the same, where the last of an item's workgroups joins its parts: how many are there; zero between calls
   __host__ __device__ Parts(char* ws, int n) {
+    arrived = reinterpret_cast<uint32_t*>(ws);
+    static_assert(kWorkgroups * sizeof(uint32_t) <= kChunkCounters, "");
+    ws += kChunkCounters;
     o = reinterpret_cast<float*>(ws);
     ml = reinterpret_cast<float2*>(ws + (size_t)n * 2 * R * D * sizeof(float));
     join = reinterpret_cast<int4*>(ws + (size_t)n * 2 * R * (D * sizeof(float) + sizeof(float2)));
   }
-  static size_t bytes(int n) { return (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
+  static size_t bytes(int n) { return kChunkCounters + (size_t)n * (2 * R * (D * sizeof(float) + sizeof(float2)) + sizeof(int4)); }
 };
 
 // Joins the parts of the items that were cut: workgroup (v, y) rows 32 y .. 32 y + 31 of the item that begins in range v.  A thread adds up four
@@ -247,8 +287,6 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
     if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
   }
 }
-
-constexpr int kWorkgroups = 256;                         // one on each compute unit
 
 }  // namespace
 

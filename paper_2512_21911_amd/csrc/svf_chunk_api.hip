@@ -148,6 +148,7 @@ int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K,
   p.max_new = shape->max_new;
   p.n_rows = shape->n_rows;
   p.window = shape->window;
+  p.unit_bound = (int64_t)shape->B * shape->Hkv * (((int64_t)shape->max_seq_len + 31) / 32 + 1);
   const float scale = shape->sm_scale > 0.f ? shape->sm_scale : 1.0f / std::sqrt((float)shape->d);
   p.scale_log2 = scale * 1.44269504088896340736f;
   const hipStream_t st = static_cast<hipStream_t>(stream);

@@ -34,6 +34,7 @@ struct ChunkParams {
   char* ws;
   int64_t q_stride, out_stride;      // elements
   int32_t B, Hq, Hkv, G, d, n_pages, max_seq_len, max_new, n_rows, window;
+  int64_t unit_bound;        // units of 32 keys that a call has at most
   float scale_log2;          // sm_scale * log2(e)
 };
 
@@ -66,6 +67,9 @@ __device__ __forceinline__ ChunkSeq chunk_seq(int len, int row, int n, int max_s
   if (s.n == 0) s.len = s.row = 0;
   return s;
 }
+
+// Bytes at the front of a workspace that count arrivals: zero between calls, whatever kernel they took
+constexpr size_t kChunkCounters = 1024;
 
 hipError_t launch_append_kv(const AppendParams& p, int dtype, hipStream_t st);
 size_t chunk_attn_workspace(const svf_chunk_shape_t& s);
