@@ -263,21 +263,22 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
       }
       __syncthreads();
       if (joins) {
-        int takers = 1;                                     // threads of a cell
-        while (2 * takers * cells <= kThreads && takers < 16) takers *= 2;
+        constexpr int kTogether = 12;                       // a trip to memory, some 2 us from another XCD, for as many parts at once
+        // (consecutive threads have consecutive cells: what a wavefront asks for at once lies side by side)
+        const int takers = cells < kThreads ? min(kThreads / cells, 16) : 1, step = takers > 1 ? cells : kThreads;
         floatx4* const others = reinterpret_cast<floatx4*>(lds);
         float2* const others_ml = reinterpret_cast<float2*>(lds + kThreads * sizeof(floatx4));
         const int parts_n = upto - from + 1;
-        for (int c0 = 0; c0 < cells; c0 += kThreads / takers) {
-          const int cell = c0 + tid / takers, first = tid % takers;
+        for (int c0 = 0; c0 < cells; c0 += step) {
+          const int first = tid / step, cell = first < takers ? c0 + tid - first * step : cells;
           const int r = (cell < cells ? cell : 0) / (D / 4), ch = 4 * (cell % (D / 4));
           float top = -INFINITY, den = 0.f;
           floatx4 y = {};
-          for (int i0 = first; i0 < parts_n; i0 += 4 * takers) {
-            float2 ml[4];
-            floatx4 z[4];
+          for (int i0 = first; i0 < parts_n; i0 += kTogether * takers) {
+            float2 ml[kTogether];
+            floatx4 z[kTogether];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kTogether; ++k) {
               const int i = min(i0 + k * takers, parts_n - 1);
               const int64_t at_part = (int64_t)(2 * (from + i) + (i == 0 ? 1 : 0)) * R + r;
               ml[k] = load_shared(&parts.ml[at_part]);
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
             }
             float now = top;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kTogether; ++k) {
               if (i0 + k * takers >= parts_n) ml[k].x = -INFINITY;
               now = fmaxf(now, ml[k].x);
             }
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
             den *= f0;
             y *= f0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kTogether; ++k)
               if (i0 + k * takers < parts_n) {
                 const float f = __builtin_amdgcn_exp2f(ml[k].x - use);
                 den += f * ml[k].y;
@@ -306,13 +307,14 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
             others_ml[tid] = make_float2(top, den);
             __syncthreads();
             if (first == 0) {
-              for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k].x);
+              for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k * step].x);
               den = 0.f;
               y = floatx4{};
               for (int k = 0; k < takers; ++k) {
-                const float f = __builtin_amdgcn_exp2f(others_ml[tid + k].x - top);
-                den += f * others_ml[tid + k].y;
-                y += f * others[tid + k];
+                const float2 ml = others_ml[tid + k * step];
+                const float f = __builtin_amdgcn_exp2f(ml.x - top);
+                den += f * ml.y;
+                y += f * others[tid + k * step];
               }
             }
             __syncthreads();
