@@ -40,21 +40,32 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), hh = lane >> 5, r32 = lane & 31;
   const Parts<D, R> parts(p.ws, gridDim.x);
 
-  int64_t* const cum = reinterpret_cast<int64_t*>(lds);
-  units_before<R, kKeys>(p, cum);
-  const int64_t total = cum[p.B];
-  const int N = (int)min((int64_t)gridDim.x, total);     // workgroups with work: one unit at least
-  // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
-  const int me = N == (int)gridDim.x ? (int)(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+  // where this workgroup's range begins
+  int64_t total = 0, at = 0, end = 0;
+  int N = 0, me = 0;
+  const auto begin = [&](int64_t all) {
+    total = all;
+    N = (int)min((int64_t)kWorkgroups, total);             // workgroups with work: one unit at least
+    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
+    me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+    at = me < N ? range_begin(total, N, me) : total;
+    end = me < N ? range_begin(total, N, me + 1) : total;
+    return at;
+  };
+  Cursor c;
+  if (!cursor_of_few<R, kKeys, false>(p, begin, c)) {
+    int64_t* const cum = reinterpret_cast<int64_t*>(lds);
+    units_before<R, kKeys>(p, cum);
+    begin(cum[p.B]);
+    if (me < N) c = cursor_at<R, kKeys>(p, cum, at);
+    __syncthreads();
+  }
   if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
   if (me >= N) return;
-  const int64_t at = range_begin(total, N, me), end = range_begin(total, N, me + 1);
-  Cursor c = cursor_at<R, kKeys>(p, cum, at);
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   c.item = uniform(c.item);
   int skip = uniform((int)c.skip), left = uniform((int)(end - at));      // units of the item in front of the range; units to do
-  __syncthreads();
 
   const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
   const bool second = wave >= kWaves / 2;
@@ -131,86 +142,66 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
 
     floatx16 sc[2];
     bf16x8 pf[4];
-    // The two products of a unit, K Q^T (scores) and V^T P^T (outputs), four instructions at a time: operands() reads the four's K or V
-    // fragments out of LDS, multiply() takes them.  V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels
+    // The two products of a unit, K Q^T (scores) and V^T P^T (outputs), kProducts instructions each.  Behind every instruction the
+    // operand of the one four further on is read, into registers that were used four before: the scheduler, left alone, puts every read right
+    // in front of its product and waits a trip to LDS for each.  V^T operands: lane 16 g + 4 j + x of a transposing read addresses channels
     // 16 (g mod 2) + 4 x .. + 3 of key j of the four keys of its half, and receives channel lane mod 16 of those keys.
-    constexpr int kGroups = D / 32;
+    constexpr int kProducts = D / 8;
     const int vt = 4 * hh + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vb = 8 * (lane & 1);
-    const auto k_operands = [&](int buf, int g, bf16x8 (&a)[4]) {
-      const char* const k = lds + buf * 2 * C::kTileBytes;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ks = 2 * g + i / 2, kk = i & 1;
-        a[i] = *reinterpret_cast<const bf16x8*>(k + C::k_at(32 * kk + r32, 2 * ks + hh));
-      }
+    const auto k_operand = [&](int buf, int i) {
+      return *reinterpret_cast<const bf16x8*>(lds + buf * 2 * C::kTileBytes + C::k_at(32 * (i & 1) + r32, 2 * (i / 2) + hh));
     };
-    const auto k_multiply = [&](int g, const bf16x8 (&a)[4]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ks = 2 * g + i / 2, kk = i & 1;
-        sc[kk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], qf[ks], ks == 0 ? floatx16{} : sc[kk], 0, 0, 0);
-      }
-    };
-    const auto v_operands = [&](int buf, int g, bf16x8 (&a)[4]) {
+    const auto v_operand = [&](int buf, int i) {
       const char* const v = lds + buf * 2 * C::kTileBytes + C::kTileBytes;
+      shortx4 h[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int kb = (4 * g + i) / (D / 32), cb = (4 * g + i) % (D / 32);
-        shortx4 x[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          x[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) shortx4*)(v + C::v_at(16 * kb + 8 * y + vt, 4 * cb + vc) + vb));
-        a[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-      }
+      for (int z = 0; z < 2; ++z)
+        h[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(
+            v + C::v_at(16 * (i / (D / 32)) + 8 * z + vt, 4 * (i % (D / 32)) + vc) + vb));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    const auto v_multiply = [&](int g, const bf16x8 (&a)[4]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int kb = (4 * g + i) / (D / 32), cb = (4 * g + i) % (D / 32);
-        o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], pf[kb], o[cb], 0, 0, 0);
-      }
+    const auto k_multiply = [&](int i, bf16x8 a) {
+      sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i / 2], i < 2 ? floatx16{} : sc[i & 1], 0, 0, 0);
     };
-    // A multiplying phase.  Operands are read four products ahead of the ones that take them (the scheduler, left alone, puts every read right
-    // in front of its product and waits a trip to LDS for each); the first four's are in `x` already.
-    bf16x8 x[4], y[4];
+    const auto v_multiply = [&](int i, bf16x8 a) {
+      const int cb = i % (D / 32);
+      o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[i / (D / 32)], o[cb], 0, 0, 0);
+    };
+    bf16x8 x[4], y[4];                                     // operands, in turn; x: of the next four products
 #define SVF_IN_ORDER() __builtin_amdgcn_sched_barrier(0x6)
-    const auto scores_after = [&](int buf) {             // (x: the first K operands)
+    const auto scores = [&](int buf) {
 #pragma unroll
-      for (int g = 0; g < kGroups; g += 2) {
-        k_operands(buf, g + 1, y);
-        SVF_IN_ORDER();
-        k_multiply(g, x);
-        SVF_IN_ORDER();
-        if (g + 2 < kGroups) k_operands(buf, g + 2, x);
-        SVF_IN_ORDER();
-        k_multiply(g + 1, y);
-        SVF_IN_ORDER();
+      for (int g = 0; g < kProducts; g += 8) {
+#pragma unroll
+        for (int i = g; i < g + 4; ++i) {
+          k_multiply(i, x[i - g]);
+          y[i - g] = k_operand(buf, i + 4);
+          SVF_IN_ORDER();
+        }
+#pragma unroll
+        for (int i = g + 4; i < g + 8; ++i) {
+          k_multiply(i, y[i - g - 4]);
+          if (i + 4 < kProducts) x[i - g - 4] = k_operand(buf, i + 4);
+          SVF_IN_ORDER();
+        }
       }
     };
-    const auto outputs_then_scores = [&](int u) {
+    const auto outputs = [&](int u) {                      // (and the scores' first operands)
 #pragma unroll
-      for (int g = 0; g < kGroups; g += 2) {
-        v_operands(u & 3, g + 1, y);
-        SVF_IN_ORDER();
-        v_multiply(g, x);
-        SVF_IN_ORDER();
-        if (g == 0 && u + 3 < n) {
-          // Loading, in the products' shadow: unit u + 3 into LDS (both have multiplied by the values of unit u - 1, which were there), u + 4
-          // on its way, u + 5 looked up
-          put((u + 3) & 3, on_way);
-          if (u + 4 < n) {
-            request(at, on_way);
-            if (u + 5 < n) look_up(u + 5, at);
-          }
+      for (int g = 0; g < kProducts; g += 8) {
+#pragma unroll
+        for (int i = g; i < g + 4; ++i) {
+          v_multiply(i, x[i - g]);
+          y[i - g] = v_operand(u & 3, i + 4);
+          SVF_IN_ORDER();
         }
-        if (g + 2 < kGroups) v_operands(u & 3, g + 2, x);
-        else k_operands((u + 1) & 3, 0, x);
-        SVF_IN_ORDER();
-        v_multiply(g + 1, y);
-        SVF_IN_ORDER();
+#pragma unroll
+        for (int i = g + 4; i < g + 8; ++i) {
+          v_multiply(i, y[i - g - 4]);
+          x[i - g - 4] = i + 4 < kProducts ? v_operand(u & 3, i + 4) : k_operand((u + 1) & 3, i + 4 - kProducts);
+          SVF_IN_ORDER();
+        }
       }
-      scores_after((u + 1) & 3);
     };
     const auto phase_ends = [&]() {
       __builtin_amdgcn_sched_barrier(0);
@@ -220,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     // A unit's scores into weights, 2^(score - m), and their sum into l.  m need not be the maximum: weights, sums and outputs are
     // floating point, and good as long as nothing overflows.  So the maximum of the first unit that a row sees serves until a unit's weights
     // sum to more than 2^40 in some row (the sums are there anyway; looking for the maximum of every unit cost a tenth of the time),
-    // and then the unit is done again with the maximum it has.  Units that need masks look for theirs.
+    // and then the unit is done again with the maximum it has.
     const auto exponents = [&](float use) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
@@ -268,18 +259,24 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     bool unseen = true;                                    // some row has seen nothing yet
     const auto weights = [&](int u) {
       const int key0 = (unit0 + u) * kKeys;
-      const bool masked = key0 + kKeys - 1 > hi_all || key0 < lo_all;
-      if (masked) {
+      if (key0 + kKeys - 1 > hi_all) {
+        const int most = hi - key0 - 4 * hh;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = key0 + 32 * kk + 8 * (i / 4) + 4 * hh + i % 4;
-            if (key > hi || key < lo) sc[kk][i] = -INFINITY;
-          }
+          for (int i = 0; i < 16; ++i)
+            if (32 * kk + 8 * (i / 4) + i % 4 > most) sc[kk][i] = -INFINITY;
+      }
+      if (key0 < lo_all) {
+        const int least = lo - key0 - 4 * hh;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (32 * kk + 8 * (i / 4) + i % 4 < least) sc[kk][i] = -INFINITY;
       }
       exponents(m == -INFINITY ? 0.f : m);
-      if (masked || unseen) {
+      if (unseen) {
         rebase();
         unseen = __ballot(m == -INFINITY) != 0;
       }
@@ -301,15 +298,28 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     // The first four wavefronts and the second four, one of each on a SIMD, are a phase apart: while the ones multiply (the outputs of a unit
     // and the scores of the next) the others work out weights.
     if (second) __syncthreads();
-    k_operands(0, 0, x);
-    scores_after(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = k_operand(0, i);
+    scores(0);
     phase_ends();
     for (int u = 0; u < n; ++u) {
       weights(u);
-      v_operands(u & 3, 0, x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = v_operand(u & 3, i);
       phase_ends();
       __builtin_amdgcn_s_setprio(2);                       // (the matrix cores first: 3 %)
-      outputs_then_scores(u);                              // (scores of nothing behind the last unit)
+      outputs(u);
+      if (u + 3 < n) {
+        // Loading, in the products' shadow: unit u + 3 into LDS (both have multiplied by the values of unit u - 1, which were there), u + 4
+        // on its way, u + 5 looked up.  (One place for all three: 957 us for 2048 tokens over 32k; among the first products 977, spread
+        // over the outputs 1179, while the weights are worked out 1116.)
+        put((u + 3) & 3, on_way);
+        if (u + 4 < n) {
+          request(at, on_way);
+          if (u + 5 < n) look_up(u + 5, at);
+        }
+      }
+      scores((u + 1) & 3);                                 // (of nothing behind the last unit)
       __builtin_amdgcn_s_setprio(0);
       phase_ends();
     }

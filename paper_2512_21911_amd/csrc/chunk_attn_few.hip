@@ -45,41 +45,26 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
   const Parts<D, R> parts(p.ws, gridDim.x);
 
   // where this workgroup's range begins
-  int64_t total, at, end;
-  Cursor c;
-  int N, me;
-  const auto place = [&]() {
-    N = (int)min((int64_t)kWorkgroups, total);
+  int64_t total = 0, at = 0, end = 0;
+  int N = 0, me = 0;
+  const auto begin = [&](int64_t all) {
+    total = all;
+    N = (int)min((int64_t)kWorkgroups, total);             // workgroups with work: one unit at least
+    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
     me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
-    at = range_begin(total, N, me);
-    end = range_begin(total, N, me + 1);
+    at = me < N ? range_begin(total, N, me) : total;
+    end = me < N ? range_begin(total, N, me + 1) : total;
+    return at;
   };
-  if (p.B <= 64 && p.unit_bound < (1 << 30)) {
-    // up to 64 sequences: lane b has sequence b, every wavefront for itself
-    const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
-    const int units = lane < p.B && s.n > 0 ? Item<R, kFewKeys>(p, s, 0).units : 0;
-    int upto = units * p.Hkv;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(upto, d, 64);
-      if (lane >= d) upto += y;
-    }
-    total = __builtin_amdgcn_readlane(upto, 63);
-    place();
-    if (me >= N) return;
-    c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
-    const int of_seq = __builtin_amdgcn_readlane(units, c.b), rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - of_seq * p.Hkv);
-    c.h = (int)((uint32_t)rest / (uint32_t)of_seq);
-    c.skip = rest - c.h * of_seq;
-  } else {
+  Cursor c;
+  if (!cursor_of_few<R, kFewKeys, true>(p, begin, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kFewKeys>(p, cum);
-    total = cum[p.B];
-    place();
-    if (me >= N) return;
-    c = cursor_at<R, kFewKeys>(p, cum, at);
+    begin(cum[p.B]);
+    if (me < N) c = cursor_at<R, kFewKeys>(p, cum, at);
     __syncthreads();
   }
+  if (me >= N) return;
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   int skip = uniform((int)c.skip), left = uniform((int)(end - at));

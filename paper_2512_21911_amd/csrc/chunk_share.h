@@ -157,6 +157,71 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
 
 constexpr int kWorkgroups = 256;                         // one on each compute unit
 
+// The same without LDS and barriers, by every wavefront for itself, where the batch has at most 64 sequences and their items (of one KV head)
+// are at most 64 in all: lane b has sequence b, then lane x item x.  `begin` says where the range begins, given the total.  ONE: no sequence
+// has more than one item.
+template <int R, int KEYS, bool ONE, typename Begin>
+__device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
+  if (p.B > 64 || p.unit_bound >= (1 << 30)) return false;
+  const int lane = threadIdx.x & 63;
+  const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
+  const int n = lane < p.B ? items_of<R>(p, s) : 0;
+  const auto scan = [&](int x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(x, d, 64);
+      if (lane >= d) x += y;
+    }
+    return x;
+  };
+  if constexpr (ONE) {
+    const int units = n > 0 ? Item<R, KEYS>(p, s, 0).units : 0, upto = scan(units * p.Hkv);
+    c.total = __builtin_amdgcn_readlane(upto, 63);
+    const int64_t at = begin(c.total);
+    if (at >= c.total) return true;                        // (nothing for this workgroup)
+    c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
+    const int of_seq = __builtin_amdgcn_readlane(units, c.b);
+    const int rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - of_seq * p.Hkv);
+    c.h = (int)((uint32_t)rest / (uint32_t)of_seq);
+    c.item = 0;
+    c.skip = rest - c.h * of_seq;
+    return true;
+  }
+  const int upto_n = scan(n);
+  if (__builtin_amdgcn_readlane(upto_n, 63) > 64) return false;
+  // lane x: the sequence of item x is the first with more than x items up to it
+  int b = 0;
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) {
+    const int y = __shfl(upto_n, b + d - 1, 64);
+    if (y <= lane) b += d;
+  }
+  const bool live = lane < __builtin_amdgcn_readlane(upto_n, 63);
+  b = live ? b : 0;
+  ChunkSeq t;
+  t.len = __shfl(s.len, b, 64);
+  t.row = 0;
+  t.n = __shfl(s.n, b, 64);
+  const int i = lane - (__shfl(upto_n, b, 64) - __shfl(n, b, 64));
+  const int upto_u = scan(live ? Item<R, KEYS>(p, t, i).units : 0);
+  // lane b again: the units of its items
+  const int last = __shfl(upto_u, max(upto_n - 1, 0), 64), before = __shfl(upto_u, max(upto_n - n - 1, 0), 64);
+  const int of_seq = n > 0 ? last - (upto_n - n > 0 ? before : 0) : 0;
+  const int upto = scan(of_seq * p.Hkv);
+  c.total = __builtin_amdgcn_readlane(upto, 63);
+  const int64_t at = begin(c.total);
+  if (at >= c.total) return true;                          // (nothing for this workgroup)
+  c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
+  const int units = __builtin_amdgcn_readlane(of_seq, c.b), rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - units * p.Hkv);
+  c.h = (int)((uint32_t)rest / (uint32_t)units);
+  const int in_head = rest - c.h * units, first = __builtin_amdgcn_readlane(upto_n, c.b) - __builtin_amdgcn_readlane(n, c.b);
+  const int front = first > 0 ? __builtin_amdgcn_readlane(upto_u, first - 1) : 0;
+  const int x = __builtin_ctzll(__ballot(lane >= first && upto_u - front > in_head));
+  c.item = x - first;
+  c.skip = in_head - (x > first ? __builtin_amdgcn_readlane(upto_u, x - 1) - front : 0);
+  return true;
+}
+
 // Loads and stores of what workgroups on different XCDs exchange: at the scope of the device, past the L2s.
 __device__ __forceinline__ void store_shared(float* p, floatx4 x) {
   const u32x4 w = __builtin_bit_cast(u32x4, x);
@@ -225,11 +290,11 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
   const int r0 = 32 * blockIdx.y, rows = min(32, it.rows - r0);
   if (rows <= 0) return;
   const int cells = rows * (D / 4);
-  int takers = 1;                                         // threads of a cell
-  while (2 * takers * cells <= kThreads && takers < 16) takers *= 2;
+  // threads of a cell; consecutive threads have consecutive cells, so that what a wavefront asks for at once lies side by side
+  const int takers = cells < kThreads ? min(kThreads / cells, 16) : 1, step = takers > 1 ? cells : kThreads;
   const int n = join.w - me + 1;
-  for (int c0 = 0; c0 < cells; c0 += kThreads / takers) {
-    const int cell = c0 + tid / takers, first = tid % takers;
+  for (int c0 = 0; c0 < cells; c0 += step) {
+    const int first = tid / step, cell = first < takers ? c0 + tid - first * step : cells;
     const bool live = cell < cells;
     const int r = r0 + (live ? cell : 0) / (D / 4), ch = 4 * (cell % (D / 4));
     float top = -INFINITY, den = 0.f;
@@ -269,13 +334,14 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
       others_ml[tid] = make_float2(top, den);
       __syncthreads();
       if (first == 0) {
-        for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k].x);
+        for (int k = 1; k < takers; ++k) top = fmaxf(top, others_ml[tid + k * step].x);
         den = 0.f;
         x = floatx4{};
         for (int k = 0; k < takers; ++k) {
-          const float f = __builtin_amdgcn_exp2f(others_ml[tid + k].x - top);
-          den += f * others_ml[tid + k].y;
-          x += f * others[tid + k];
+          const float2 ml = others_ml[tid + k * step];
+          const float f = __builtin_amdgcn_exp2f(ml.x - top);
+          den += f * ml.y;
+          x += f * others[tid + k * step];
         }
       }
     }
