@@ -14,7 +14,7 @@ CALLS_PATH = os.path.join(PKG_DIR, "_svf_calls.so")
 
 SOURCES = ["svf_api.hip", "block_reps.hip", "score_select.hip", "verify_attn_f32.hip", "verify_attn_mfma.hip",
            "analytics.hip", "retrieve.hip", "sparse_ffn.hip", "svf_ffn_api.hip", "spec_rules.hip", "svf_chunk_api.hip", "append_kv.hip",
-           "chunk_attn.hip", "chunk_attn_few.hip", "chunk_attn_f32.hip", "sample.hip"]
+           "chunk_attn.hip", "chunk_attn_few.hip", "sample.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

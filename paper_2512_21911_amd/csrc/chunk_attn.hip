@@ -7,7 +7,8 @@ namespace svf {
 
 namespace {
 
-constexpr int kKeys = 64;                                // keys of a unit
+constexpr int kKeys = 64;                                // keys of a unit: 2 us
+constexpr int kExtra = 4;                                // an item's beginning and end: 8 us
 
 template <int D>
 struct Kernel {
@@ -53,11 +54,11 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kKeys, false>(p, begin, c)) {
+  if (!cursor_of_few<R, kKeys, kExtra, false>(p, begin, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
-    units_before<R, kKeys>(p, cum);
+    units_before<R, kKeys, kExtra>(p, cum);
     begin(cum[p.B]);
-    if (me < N) c = cursor_at<R, kKeys>(p, cum, at);
+    if (me < N) c = cursor_at<R, kKeys, kExtra>(p, cum, at);
     __syncthreads();
   }
   if (tid == 0) parts.join[me] = make_int4(-1, 0, 0, 0);
@@ -65,16 +66,17 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   c.item = uniform(c.item);
-  int skip = uniform((int)c.skip), left = uniform((int)(end - at));      // units of the item in front of the range; units to do
+  int skip = uniform((int)c.skip), left = uniform((int)(end - at));      // shares of the item in front of the range; shares to do
 
   const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
   const bool second = wave >= kWaves / 2;
-  while (left > 0) {
+  while (skip + left > kExtra) {                             // (else the range ends in front of an item's units)
     ChunkSeq s = load_seq(p, c.b);
     s = {uniform(s.len), uniform(s.row), uniform(s.n)};
-    const Item<R, kKeys> it(p, s, c.item);
-    const int n = min(it.units - skip, left);              // units of this item in the range
-    const int unit0 = it.unit0 + skip;
+    const Item<R, kKeys, kExtra> it(p, s, c.item);
+    const Part part(it, skip, left);
+    const int n = part.end - part.begin, unit0 = it.unit0 + part.begin;
+    const int64_t first_unit = end - left - skip + kExtra;   // (counted in shares) of the item
     const char* const K = static_cast<const char*>(p.K) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
     const char* const V = static_cast<const char*>(p.V) + 2 * (int64_t)c.h * p.kv.stride_head + 16 * c_lane;
 
@@ -168,7 +170,6 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[i / (D / 32)], o[cb], 0, 0, 0);
     };
     bf16x8 x[4], y[4];                                     // operands, in turn; x: of the next four products
-#define SVF_IN_ORDER() __builtin_amdgcn_sched_barrier(0x6)
     const auto scores = [&](int buf) {
 #pragma unroll
       for (int g = 0; g < kProducts; g += 8) {
@@ -326,16 +327,12 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     if (!second) __syncthreads();
 
     // this item's result, whole or a part
-    const bool begins = skip == 0, ends = skip + n == it.units;
-    const int part = begins ? 1 : 0;
-    if (begins && !ends && tid == 0) {
-      const int64_t last_unit = end - left + it.units - 1;
-      parts.join[me] = make_int4(c.b, c.h, c.item, owner_of(total, N, last_unit));
-    }
+    if (part.begins && !part.ends && tid == 0)
+      parts.join[me] = make_int4(c.b, c.h, c.item, owner_of(total, N, first_unit + it.units - 1));
     const int r = wave * 32 + r32;
     const float den = halves_sum(l);
     if (r < it.rows) {
-      if (begins && ends) {
+      if (part.begins && part.ends) {
         const int head = c.h * p.G + row - row_j * p.G;
         const float inv = 1.0f / den;
         char* to = static_cast<char*>(p.out) + 2 * ((int64_t)(s.row + row_j) * p.out_stride + (int64_t)head * D) + 8 * hh;
@@ -349,7 +346,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
           }
         if (p.lse && hh == 0) p.lse[(int64_t)(s.row + row_j) * p.Hq + head] = (m + log2f(den)) * 0.69314718055994530942f;
       } else {
-        const int64_t at_part = (int64_t)(2 * me + part) * R + r;
+        const int64_t at_part = (int64_t)(2 * me + (part.begins ? 1 : 0)) * R + r;
         float* to = parts.o + at_part * D + 4 * hh;
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)
@@ -363,14 +360,14 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     }
 
     // the next item
-    left -= n;
+    left -= part.taken;
     skip = 0;
     if (++c.item == items_of<R>(p, s)) {
       c.item = 0;
       if (++c.h == p.Hkv) {
         c.h = 0;
         ++c.b;
-        while (left > 0 && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with units: some are left)
+        while (left > 0 && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with shares: some are left)
       }
     }
   }
@@ -380,20 +377,18 @@ template <int D>
 hipError_t launch_d(const ChunkParams& p, hipStream_t st) {
   typedef Kernel<D> C;
   hipLaunchKernelGGL(chunk_attn_kernel<D>, dim3(kWorkgroups), dim3(kThreads), 0, st, p);
-  hipLaunchKernelGGL((chunk_merge_kernel<D, C::R, kKeys>), dim3(kWorkgroups, (unsigned)std::min<int64_t>(C::R / 32, ((int64_t)p.max_new * p.G + 31) / 32)),
+  hipLaunchKernelGGL((chunk_merge_kernel<D, C::R, kKeys, kExtra>), dim3(kWorkgroups, (unsigned)std::min<int64_t>(C::R / 32, ((int64_t)p.max_new * p.G + 31) / 32)),
                      dim3(kThreads), 0, st, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t chunk_attn_workspace(const svf_chunk_shape_t& s) {
-  if (chunk_attn_is_few(s.Hq / s.Hkv, s.max_new)) return chunk_attn_few_workspace(s.d);
-  return s.d == 128 ? Parts<128, Kernel<128>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64>::R>::bytes(kWorkgroups);
+size_t chunk_attn_workspace(int d) {
+  return d == 128 ? Parts<128, Kernel<128>::R>::bytes(kWorkgroups) : Parts<64, Kernel<64>::R>::bytes(kWorkgroups);
 }
 
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st) {
-  if (chunk_attn_is_few(p.G, p.max_new)) return launch_chunk_attn_few(p, st);
   return p.d == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
 }
 

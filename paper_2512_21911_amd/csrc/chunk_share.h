@@ -19,6 +19,9 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
 
+// Nothing but arithmetic is moved across this by the scheduler
+#define SVF_IN_ORDER() __builtin_amdgcn_sched_barrier(0x6)
+
 constexpr int kThreads = 512, kWaves = 8;
 constexpr int kMostB = 4096;
 constexpr int kXcds = 8;
@@ -37,10 +40,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // One item: R query rows (row r = query head r % G of new token r / G) of a (sequence, KV head) against the
-// units of KEYS keys that they see.
-template <int R, int KEYS>
+// units of KEYS keys that they see.  Work is shared out by its cost: an item counts as many shares as it has units, and EXTRA in front of them for
+// its beginning and end (reads in a chain, queries, a result), so that a range of many short items is no longer than one of a long one.
+template <int R, int KEYS, int EXTRA>
 struct Item {
-  int row0, rows, first, last, unit0, units;
+  int row0, rows, first, last, unit0, units, shares;
   __device__ __forceinline__ Item(const ChunkParams& p, const ChunkSeq& s, int i) {
     const int M = s.n * p.G;
     row0 = i * R;
@@ -50,6 +54,7 @@ struct Item {
     last = s.len + j1;
     unit0 = first / KEYS;
     units = last / KEYS + 1 - unit0;
+    shares = units + EXTRA;
   }
 };
 template <int R>
@@ -79,35 +84,35 @@ __device__ __forceinline__ int64_t wave_scan64(int64_t x, int lane) {
   return x;
 }
 
-// Units of all items of one KV head of a sequence, by a wavefront.
-template <int R, int KEYS>
+// Shares of all items of one KV head of a sequence, by a wavefront.
+template <int R, int KEYS, int EXTRA>
 __device__ int64_t units_of_seq(const ChunkParams& p, const ChunkSeq& s, int lane) {
   const int n = items_of<R>(p, s);
   int64_t sum = 0;
-  for (int i = lane; i < n; i += 64) sum += Item<R, KEYS>(p, s, i).units;
+  for (int i = lane; i < n; i += 64) sum += Item<R, KEYS, EXTRA>(p, s, i).shares;
   return lane64(wave_scan64(sum, lane), 63);
 }
 
-// How the work of a call is shared: all units of all items in a row (sequence, KV head, item, unit), cut into as many
+// How the work of a call is shared: all shares of all items in a row (sequence, KV head, item, share), cut into as many
 // equal ranges as there are workgroups.
 struct Cursor {
   int b, h, item;            // where a range begins
-  int64_t skip;              // units of that item in front of it
+  int64_t skip;              // shares of that item in front of it
   int64_t total;
 };
 // cum: [kMostB + 1] in LDS
-template <int R, int KEYS>
+template <int R, int KEYS, int EXTRA>
 __device__ void units_before(const ChunkParams& p, int64_t* cum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int b = threadIdx.x; b < p.B; b += kThreads) {
     const ChunkSeq s = load_seq(p, b);
     const int n = items_of<R>(p, s);
-    cum[b + 1] = n == 0 ? 0 : n == 1 ? Item<R, KEYS>(p, s, 0).units : -1;
+    cum[b + 1] = n == 0 ? 0 : n == 1 ? Item<R, KEYS, EXTRA>(p, s, 0).shares : -1;
   }
   __syncthreads();
   for (int b = wave; b < p.B; b += kWaves) {
     if (cum[b + 1] >= 0) continue;
-    const int64_t u = units_of_seq<R, KEYS>(p, load_seq(p, b), lane);
+    const int64_t u = units_of_seq<R, KEYS, EXTRA>(p, load_seq(p, b), lane);
     if (lane == 0) cum[b + 1] = u;
   }
   __syncthreads();
@@ -122,7 +127,7 @@ __device__ void units_before(const ChunkParams& p, int64_t* cum) {
   }
   __syncthreads();
 }
-template <int R, int KEYS>
+template <int R, int KEYS, int EXTRA>
 __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at) {
   const int lane = threadIdx.x & 63;
   Cursor c;
@@ -141,7 +146,7 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
   const int n = items_of<R>(p, s);
   c.item = 0;
   for (int i0 = 0;; i0 += 64) {
-    const int64_t x = wave_scan64(i0 + lane < n ? Item<R, KEYS>(p, s, i0 + lane).units : 0, lane);
+    const int64_t x = wave_scan64(i0 + lane < n ? Item<R, KEYS, EXTRA>(p, s, i0 + lane).shares : 0, lane);
     const uint64_t in = __ballot(rest < x);
     if (in) {
       const int l = __builtin_ctzll(in);
@@ -160,7 +165,7 @@ constexpr int kWorkgroups = 256;                         // one on each compute 
 // The same without LDS and barriers, by every wavefront for itself, where the batch has at most 64 sequences and their items (of one KV head)
 // are at most 64 in all: lane b has sequence b, then lane x item x.  `begin` says where the range begins, given the total.  ONE: no sequence
 // has more than one item.
-template <int R, int KEYS, bool ONE, typename Begin>
+template <int R, int KEYS, int EXTRA, bool ONE, typename Begin>
 __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
   if (p.B > 64 || p.unit_bound >= (1 << 30)) return false;
   const int lane = threadIdx.x & 63;
@@ -175,7 +180,7 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
     return x;
   };
   if constexpr (ONE) {
-    const int units = n > 0 ? Item<R, KEYS>(p, s, 0).units : 0, upto = scan(units * p.Hkv);
+    const int units = n > 0 ? Item<R, KEYS, EXTRA>(p, s, 0).shares : 0, upto = scan(units * p.Hkv);
     c.total = __builtin_amdgcn_readlane(upto, 63);
     const int64_t at = begin(c.total);
     if (at >= c.total) return true;                        // (nothing for this workgroup)
@@ -203,7 +208,7 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
   t.row = 0;
   t.n = __shfl(s.n, b, 64);
   const int i = lane - (__shfl(upto_n, b, 64) - __shfl(n, b, 64));
-  const int upto_u = scan(live ? Item<R, KEYS>(p, t, i).units : 0);
+  const int upto_u = scan(live ? Item<R, KEYS, EXTRA>(p, t, i).shares : 0);
   // lane b again: the units of its items
   const int last = __shfl(upto_u, max(upto_n - 1, 0), 64), before = __shfl(upto_u, max(upto_n - n - 1, 0), 64);
   const int of_seq = n > 0 ? last - (upto_n - n > 0 ? before : 0) : 0;
@@ -245,7 +250,7 @@ __device__ __forceinline__ float2 load_shared(const float2* p) {
   return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
 }
 
-// Workgroup v of n takes units [range_begin(v), range_begin(v + 1)); n is kWorkgroups, or the number of units if that is less.
+// Workgroup v of n takes shares [range_begin(v), range_begin(v + 1)); n is kWorkgroups, or the number of shares if that is less.
 __device__ __forceinline__ int64_t range_begin(int64_t total, int n, int v) {
   return n == kWorkgroups ? (total * v) / kWorkgroups : (int64_t)v;
 }
@@ -255,6 +260,21 @@ __device__ __forceinline__ int owner_of(int64_t total, int n, int64_t unit) {
   if (total < (1 << 22)) return (int)((uint32_t)((unit + 1) * kWorkgroups - 1) / (uint32_t)total);
   return (int)(((unit + 1) * kWorkgroups - 1) / total);
 }
+
+// The part of an item that shares [skip, skip + left) of it are: units [begin, end); it begins or ends the item, or is all of it.  `from`, `upto`: the
+// workgroups that have the item's first and last unit.
+struct Part {
+  int taken, begin, end;
+  bool begins, ends;
+  template <int R, int KEYS, int EXTRA>
+  __device__ __forceinline__ Part(const Item<R, KEYS, EXTRA>& it, int skip, int left) {
+    taken = min(it.shares - skip, left);
+    begin = max(skip - EXTRA, 0);
+    end = max(skip + taken - EXTRA, 0);
+    begins = begin == 0;
+    ends = end == it.units;
+  }
+};
 
 // The workspace: for every workgroup two partial results of R rows (0: of the item its range begins inside of, 1: of the one
 // its range ends inside of) and what the second launch joins.
@@ -277,7 +297,7 @@ struct Parts {
 
 // Joins the parts of the items that were cut: workgroup (v, y) rows 32 y .. 32 y + 31 of the item that begins in range v.  A thread adds up four
 // channels of a row; where rows are few, several threads take the parts in turn.
-template <int D, int R, int KEYS>
+template <int D, int R, int KEYS, int EXTRA>
 __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
   __shared__ floatx4 others[kThreads];
   __shared__ float2 others_ml[kThreads];
@@ -286,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void chunk_merge_kernel(ChunkParams p) {
   const int4 join = parts.join[me];
   if (join.x < 0) return;
   const ChunkSeq s = load_seq(p, join.x);
-  const Item<R, KEYS> it(p, s, join.z);
+  const Item<R, KEYS, EXTRA> it(p, s, join.z);
   const int r0 = 32 * blockIdx.y, rows = min(32, it.rows - r0);
   if (rows <= 0) return;
   const int cells = rows * (D / 4);

@@ -53,8 +53,12 @@ svf::KvLayout layout_of(const svf_chunk_shape_t& s) {
   return kv;
 }
 
+// (the choice between the kernels: single tokens are bound by memory, which the one for few rows keeps busier: 108 against 169 us for four
+// tokens over 32k; it takes 32 rows)
+bool few_rows(const svf_chunk_shape_t& s) { return s.dtype == SVF_F32 || svf::chunk_attn_is_few(s.Hq / s.Hkv, s.max_new); }
+
 size_t workspace_of(const svf_chunk_shape_t& s) {
-  const size_t n = s.dtype == SVF_F32 ? svf::chunk_attn_f32_workspace(s) : svf::chunk_attn_workspace(s);
+  const size_t n = few_rows(s) ? svf::chunk_attn_few_workspace(s.d) : svf::chunk_attn_workspace(s.d);
   return (n + kAlign - 1) / kAlign * kAlign;
 }
 
@@ -152,7 +156,7 @@ int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K,
   const float scale = shape->sm_scale > 0.f ? shape->sm_scale : 1.0f / std::sqrt((float)shape->d);
   p.scale_log2 = scale * 1.44269504088896340736f;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return (shape->dtype == SVF_F32 ? svf::launch_chunk_attn_f32(p, st) : svf::launch_chunk_attn(p, st)) == hipSuccess
+  return (few_rows(*shape) ? svf::launch_chunk_attn_few(p, shape->dtype == SVF_F32, st) : svf::launch_chunk_attn(p, st)) == hipSuccess
              ? SVF_OK : SVF_ERR_HIP;
 }
 

@@ -72,13 +72,11 @@ __device__ __forceinline__ ChunkSeq chunk_seq(int len, int row, int n, int max_s
 constexpr size_t kChunkCounters = 1024;
 
 hipError_t launch_append_kv(const AppendParams& p, int dtype, hipStream_t st);
-size_t chunk_attn_workspace(const svf_chunk_shape_t& s);
+size_t chunk_attn_workspace(int d);
 hipError_t launch_chunk_attn(const ChunkParams& p, hipStream_t st);
-// few rows per (sequence, KV head): a kernel of its own
+// 32 rows of a (sequence, KV head) at a time: bf16 with no more of them, and fp32
 bool chunk_attn_is_few(int G, int max_new);
 size_t chunk_attn_few_workspace(int d);
-hipError_t launch_chunk_attn_few(const ChunkParams& p, hipStream_t st);
-size_t chunk_attn_f32_workspace(const svf_chunk_shape_t& s);
-hipError_t launch_chunk_attn_f32(const ChunkParams& p, hipStream_t st);
+hipError_t launch_chunk_attn_few(const ChunkParams& p, bool f32, hipStream_t st);
 
 }  // namespace svf
