@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kKeys, kExtra, false>(p, begin, c)) {
+  if (!cursor_of_few<R, kKeys, kExtra>(p, begin, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kKeys, kExtra>(p, cum);
     begin(cum[p.B]);

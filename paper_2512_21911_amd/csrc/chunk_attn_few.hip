@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kFewKeys, kExtra, E == 2>(p, begin, c)) {
+  if (!cursor_of_few<R, kFewKeys, kExtra>(p, begin, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kFewKeys, kExtra>(p, cum);
     begin(cum[p.B]);
@@ -341,8 +341,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
     const bool whole = part.begins && part.ends;
     const int from = whole ? me : owner_of(total, N, first_unit), upto = whole ? me : owner_of(total, N, first_unit + it.units - 1);
     const auto write = [&](int r, int ch, float top, float den, floatx4 y) {
+      const float inv = 1.0f / den;
       const int at_row = it.row0 + r, j = at_row / p.G, head = c.h * p.G + at_row - j * p.G;
-      Unit::write(static_cast<char*>(p.out) + E * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch), y / den);
+      Unit::write(static_cast<char*>(p.out) + E * ((int64_t)(s.row + j) * p.out_stride + (int64_t)head * D + ch), y * inv);
       if (ch == 0 && p.lse) p.lse[(int64_t)(s.row + j) * p.Hq + head] = (top + log2f(den)) * 0.69314718055994530942f;
     };
     const int cells = it.rows * (D / 4);

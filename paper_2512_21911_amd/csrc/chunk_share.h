@@ -162,68 +162,63 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
 
 constexpr int kWorkgroups = 256;                         // one on each compute unit
 
-// The same without LDS and barriers, by every wavefront for itself, where the batch has at most 64 sequences and their items (of one KV head)
-// are at most 64 in all: lane b has sequence b, then lane x item x.  `begin` says where the range begins, given the total.  ONE: no sequence
-// has more than one item.
-template <int R, int KEYS, int EXTRA, bool ONE, typename Begin>
+// Sums of whole numbers of units.  T = R / G tokens of an item and KEYS are powers of two (shifts t and k).
+// sum over x < n of (b + x T) / KEYS, rounded down
+__device__ __forceinline__ int sum_of_units(int b, int n, int t, int k) {
+  if (t >= k) return n * (b >> k) + ((n * (n - 1) / 2) << (t - k));
+  const int q = k - t, s = b >> t;                         // the same as of (s + x) / 2^q
+  const auto upto = [&](int x) {
+    const int d = x >> q;
+    return ((d * (d - 1) / 2) << q) + d * (x - (d << q));
+  };
+  return upto(s + n) - upto(s);
+}
+// Shares of the first i items of one KV head of a sequence.
+template <int R, int KEYS, int EXTRA>
+__device__ __forceinline__ int shares_upto(const ChunkParams& p, const ChunkSeq& s, int i) {
+  constexpr int k = __builtin_ctz(KEYS);
+  const int t = __builtin_ctz(R) - __builtin_ctz(p.G), T = 1 << t;
+  const int items = items_of<R>(p, s), full = min(i, items - 1);         // (the last may have fewer rows)
+  if (items == 0) return 0;
+  int sum = full * (1 + EXTRA) + sum_of_units(s.len + T - 1, full, t, k);
+  if (p.window > 0) {                                                    // less the units in front of the first tokens' windows
+    const int c = s.len + 1 - p.window, x0 = c < 0 ? min(full, (-c + T - 1) >> t) : 0;
+    sum -= sum_of_units(max(c + (x0 << t), 0), full - x0, t, k);
+  }
+  return i > full ? sum + Item<R, KEYS, EXTRA>(p, s, items - 1).shares : sum;
+}
+
+// The same without LDS and barriers, by every wavefront for itself, for up to 64 sequences (lane b has sequence b) and groups of a power of two
+// of query heads, whose items' units have a sum in closed form.  `begin` says where the range begins, given the total.
+template <int R, int KEYS, int EXTRA, typename Begin>
 __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
-  if (p.B > 64 || p.unit_bound >= (1 << 30)) return false;
+  if (p.B > 64 || p.share_bound >= (1 << 30) || (p.G & (p.G - 1)) != 0 || p.G > R) return false;
   const int lane = threadIdx.x & 63;
   const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
-  const int n = lane < p.B ? items_of<R>(p, s) : 0;
-  const auto scan = [&](int x) {
+  const int n = lane < p.B ? items_of<R>(p, s) : 0, of_seq = n > 0 ? shares_upto<R, KEYS, EXTRA>(p, s, n) : 0;
+  int upto = of_seq * p.Hkv;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(x, d, 64);
-      if (lane >= d) x += y;
-    }
-    return x;
-  };
-  if constexpr (ONE) {
-    const int units = n > 0 ? Item<R, KEYS, EXTRA>(p, s, 0).shares : 0, upto = scan(units * p.Hkv);
-    c.total = __builtin_amdgcn_readlane(upto, 63);
-    const int64_t at = begin(c.total);
-    if (at >= c.total) return true;                        // (nothing for this workgroup)
-    c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
-    const int of_seq = __builtin_amdgcn_readlane(units, c.b);
-    const int rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - of_seq * p.Hkv);
-    c.h = (int)((uint32_t)rest / (uint32_t)of_seq);
-    c.item = 0;
-    c.skip = rest - c.h * of_seq;
-    return true;
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += y;
   }
-  const int upto_n = scan(n);
-  if (__builtin_amdgcn_readlane(upto_n, 63) > 64) return false;
-  // lane x: the sequence of item x is the first with more than x items up to it
-  int b = 0;
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) {
-    const int y = __shfl(upto_n, b + d - 1, 64);
-    if (y <= lane) b += d;
-  }
-  const bool live = lane < __builtin_amdgcn_readlane(upto_n, 63);
-  b = live ? b : 0;
-  ChunkSeq t;
-  t.len = __shfl(s.len, b, 64);
-  t.row = 0;
-  t.n = __shfl(s.n, b, 64);
-  const int i = lane - (__shfl(upto_n, b, 64) - __shfl(n, b, 64));
-  const int upto_u = scan(live ? Item<R, KEYS, EXTRA>(p, t, i).shares : 0);
-  // lane b again: the units of its items
-  const int last = __shfl(upto_u, max(upto_n - 1, 0), 64), before = __shfl(upto_u, max(upto_n - n - 1, 0), 64);
-  const int of_seq = n > 0 ? last - (upto_n - n > 0 ? before : 0) : 0;
-  const int upto = scan(of_seq * p.Hkv);
   c.total = __builtin_amdgcn_readlane(upto, 63);
   const int64_t at = begin(c.total);
   if (at >= c.total) return true;                          // (nothing for this workgroup)
   c.b = __builtin_ctzll(__ballot((int64_t)upto > at));
-  const int units = __builtin_amdgcn_readlane(of_seq, c.b), rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - units * p.Hkv);
-  c.h = (int)((uint32_t)rest / (uint32_t)units);
-  const int in_head = rest - c.h * units, first = __builtin_amdgcn_readlane(upto_n, c.b) - __builtin_amdgcn_readlane(n, c.b);
-  const int front = first > 0 ? __builtin_amdgcn_readlane(upto_u, first - 1) : 0;
-  const int x = __builtin_ctzll(__ballot(lane >= first && upto_u - front > in_head));
-  c.item = x - first;
-  c.skip = in_head - (x > first ? __builtin_amdgcn_readlane(upto_u, x - 1) - front : 0);
+  const int per_head = __builtin_amdgcn_readlane(of_seq, c.b);
+  int rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - per_head * p.Hkv);
+  c.h = (int)((uint32_t)rest / (uint32_t)per_head);
+  rest -= c.h * per_head;
+  const ChunkSeq t{__builtin_amdgcn_readlane(s.len, c.b), 0, __builtin_amdgcn_readlane(s.n, c.b)};
+  int lo = 0, hi = __builtin_amdgcn_readlane(n, c.b) - 1;  // the last item with no more than `rest` shares in front of it
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (shares_upto<R, KEYS, EXTRA>(p, t, mid) <= rest) lo = mid;
+    else hi = mid - 1;
+  }
+  c.item = lo;
+  c.skip = rest - shares_upto<R, KEYS, EXTRA>(p, t, lo);
   return true;
 }
 

@@ -152,7 +152,9 @@ int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K,
   p.max_new = shape->max_new;
   p.n_rows = shape->n_rows;
   p.window = shape->window;
-  p.unit_bound = (int64_t)shape->B * shape->Hkv * (((int64_t)shape->max_seq_len + 31) / 32 + 1);
+  // (items of 32 rows, units of 32 keys, no more than sixteen shares beside them; up to 2^24 of both each: no overflow below 2^62)
+  const int64_t share_items = ((int64_t)shape->max_new * p.G + 31) / 32, share_units = (int64_t)shape->max_seq_len / 32 + 18;
+  p.share_bound = share_items > (1 << 30) / share_units ? INT64_MAX : (int64_t)shape->B * shape->Hkv * share_items * share_units;
   const float scale = shape->sm_scale > 0.f ? shape->sm_scale : 1.0f / std::sqrt((float)shape->d);
   p.scale_log2 = scale * 1.44269504088896340736f;
   const hipStream_t st = static_cast<hipStream_t>(stream);

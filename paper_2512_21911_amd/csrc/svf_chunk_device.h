@@ -34,7 +34,7 @@ struct ChunkParams {
   char* ws;
   int64_t q_stride, out_stride;      // elements
   int32_t B, Hq, Hkv, G, d, n_pages, max_seq_len, max_new, n_rows, window;
-  int64_t unit_bound;        // units of 32 keys that a call has at most
+  int64_t share_bound;       // shares of work (chunk_share.h) that a call has at most
   float scale_log2;          // sm_scale * log2(e)
 };
 
