@@ -162,14 +162,17 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
 
 constexpr int kWorkgroups = 256;                         // one on each compute unit
 
-// Sums of whole numbers of units.  T = R / G tokens of an item and KEYS are powers of two (shifts t and k).
+// Sums of whole numbers of units.  T = R / G tokens of an item and KEYS are powers of two (shifts t and k).  Terms may pass 2^32 where the
+// result doesn't (a million tokens in front, few tokens an item): everything is counted modulo 2^32.
 // sum over x < n of (b + x T) / KEYS, rounded down
-__device__ __forceinline__ int sum_of_units(int b, int n, int t, int k) {
-  if (t >= k) return n * (b >> k) + ((n * (n - 1) / 2) << (t - k));
-  const int q = k - t, s = b >> t;                         // the same as of (s + x) / 2^q
-  const auto upto = [&](int x) {
-    const int d = x >> q;
-    return ((d * (d - 1) / 2) << q) + d * (x - (d << q));
+__device__ __forceinline__ uint32_t sum_of_units(uint32_t b, uint32_t n, int t, int k) {
+  const auto pairs = [](uint32_t d) { return (d >> 1) * ((d - 1) | 1); };     // d (d - 1) / 2
+  if (t >= k) return n * (b >> k) + (pairs(n) << (t - k));
+  const int q = k - t;
+  const uint32_t s = b >> t;                               // the same as of (s + x) / 2^q
+  const auto upto = [&](uint32_t x) {
+    const uint32_t d = x >> q;
+    return (pairs(d) << q) + d * (x - (d << q));
   };
   return upto(s + n) - upto(s);
 }
@@ -180,12 +183,12 @@ __device__ __forceinline__ int shares_upto(const ChunkParams& p, const ChunkSeq&
   const int t = __builtin_ctz(R) - __builtin_ctz(p.G), T = 1 << t;
   const int items = items_of<R>(p, s), full = min(i, items - 1);         // (the last may have fewer rows)
   if (items == 0) return 0;
-  int sum = full * (1 + EXTRA) + sum_of_units(s.len + T - 1, full, t, k);
+  uint32_t sum = full * (1 + EXTRA) + sum_of_units(s.len + T - 1, full, t, k);
   if (p.window > 0) {                                                    // less the units in front of the first tokens' windows
     const int c = s.len + 1 - p.window, x0 = c < 0 ? min(full, (-c + T - 1) >> t) : 0;
     sum -= sum_of_units(max(c + (x0 << t), 0), full - x0, t, k);
   }
-  return i > full ? sum + Item<R, KEYS, EXTRA>(p, s, items - 1).shares : sum;
+  return (int)(i > full ? sum + Item<R, KEYS, EXTRA>(p, s, items - 1).shares : sum);
 }
 
 // The same without LDS and barriers, by every wavefront for itself, for up to 64 sequences (lane b has sequence b) and groups of a power of two

@@ -39,6 +39,7 @@ constexpr int kPlaceBits = 31;                           // of a weight relative
 constexpr int kCountAt = 47;                             // a histogram's word: 2^15 such weights, and above them how many
 constexpr int kBins = 1024;                              // the last: everything below the others
 constexpr int kList = 4096;                              // tokens around the border that are sorted
+constexpr float kFar = 3e38f;                            // bins of logits further from zero are this one
 constexpr double kLog2e = 1.4426950408889634074;
 
 struct SliceStats {
@@ -92,21 +93,41 @@ __device__ __forceinline__ float4 load4(const __hip_bfloat16* p) {
 }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __hip_bfloat16* p) { return __bfloat162float(*p); }
+// (NaN alone; no more than a maximum takes)
+__device__ __forceinline__ float number(float x) { return fmaxf(x, -INFINITY); }
 // tokens v .. v + 3, -inf past the end
 template <typename T>
 __device__ __forceinline__ float4 logits4(const T* x, int v, int end) {
   float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-  if (v + 3 < end) {
-    f = load4(x + v);
-  } else {
-    if (v < end) f.x = load1(x + v);
-    if (v + 1 < end) f.y = load1(x + v + 1);
-    if (v + 2 < end) f.z = load1(x + v + 2);
+  if (v < end) f.x = load1(x + v);
+  if (v + 1 < end) f.y = load1(x + v + 1);
+  if (v + 2 < end) f.z = load1(x + v + 2);
+  if (v + 3 < end) f.w = load1(x + v + 3);
+  return f;
+}
+struct Clean { __device__ __forceinline__ float operator()(float x) const { return clean(x); } };
+struct Number { __device__ __forceinline__ float operator()(float x) const { return number(x); } };
+// Tokens v0 + 4 (i THREADS + thread) .. + 3 of all i < N.  Whether all threads' are inside the row is the same for the workgroup, and then the
+// loads are under no mask: under one they wait for each other (16.9 us instead of 13.x for the first launch at 64 rows of 129 280).
+template <int N, int THREADS, typename Each = Clean, typename T>
+__device__ __forceinline__ void read_logits(const T* x, int v0, int thread, int end, float4 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int v = v0 + 4 * i * THREADS;
+    if (v + 4 * THREADS <= end) f[i] = load4(x + v + 4 * thread);
+    else f[i] = logits4(x, v + 4 * thread, end);
   }
-  return make_float4(clean(f.x), clean(f.y), clean(f.z), clean(f.w));
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = make_float4(Each()(f[i].x), Each()(f[i].y), Each()(f[i].z), Each()(f[i].w));
 }
 __device__ __forceinline__ float get(const float4& f, int i) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+
+// the smallest fp32 number that is no less
+__device__ __forceinline__ float at_least(double x) {
+  const float f = (float)x;
+  return (double)f < x ? nextafterf(f, INFINITY) : f;
+}
 
 // ---- a row's settings ------------------------------------------------------------------------------
 
@@ -136,7 +157,7 @@ struct Settings {
   __device__ __forceinline__ bool filtered() const { return k > 0 || top_p < 1.f || min_p > 0.f; }
   // the bin's number (from the logits' zero up; whole) and the place in it, 0 <= place < 1: both exact
   __device__ __forceinline__ float bin_of(float x, float& place) const {
-    const float at = fminf(fmaxf(x * per_bin, -3e38f), 3e38f), b = floorf(at);
+    const float at = __builtin_amdgcn_fmed3f(x * per_bin, -kFar, kFar), b = floorf(at);   // (x is no NaN)
     place = at - b;
     return b;
   }
@@ -147,24 +168,27 @@ struct Settings {
   __device__ __forceinline__ uint32_t least_key(float top) const {
     if (min_p == 0.f) return 0;
     const double least = (double)top + (double)temperature * log((double)min_p);
-    float f = (float)least;
-    if ((double)f < least) f = nextafterf(f, INFINITY);
-    return score_key(fminf(f, top));
+    return score_key(fminf(at_least(least), top));
   }
 };
 
 // ---- weights ---------------------------------------------------------------------------------------
 
-// 2^(place bin_log2) - 1; z = bin_log2 ln 2 <= 1/32
-__device__ __forceinline__ float place_excess(float place, float z) {
-  const float x = place * z;
-  return x * (1.f + x * (0.5f + x * (1.f / 6.f + x * (1.f / 24.f))));
-}
-__device__ __forceinline__ float place_factor(const Settings& set) { return (float)(set.bin_log2 * 0.69314718055994530942); }
-// the same in fixed point, the one included
-__device__ __forceinline__ uint32_t place_weight(float place, float z) {
-  return (1u << kPlaceBits) + (uint32_t)(place_excess(place, z) * (float)(1u << kPlaceBits));
-}
+// 2^(place bin_log2) - 1 times `scale`: four terms of the series, z = bin_log2 ln 2 <= 1/32
+struct PlaceExcess {
+  float c1, c2, c3, c4;
+  __device__ __forceinline__ explicit PlaceExcess(const Settings& set, float scale = 1.f) {
+    const float z = (float)(set.bin_log2 * 0.69314718055994530942);
+    c1 = z * scale;
+    c2 = c1 * z * 0.5f;
+    c3 = c2 * z * (1.f / 3.f);
+    c4 = c3 * z * 0.25f;
+  }
+  __device__ __forceinline__ float operator()(float place) const { return place * (c1 + place * (c2 + place * (c3 + place * c4))); }
+};
+// 2^(place bin_log2) in fixed point; of an excess scaled by kPlaceOne
+constexpr float kPlaceOne = (float)(1u << kPlaceBits);
+__device__ __forceinline__ uint32_t place_weight(float place, const PlaceExcess& excess) { return (1u << kPlaceBits) + (uint32_t)excess(place); }
 // 2^t, t <= 0: ten terms of the series around the nearest whole number, 2^-36 relative
 __device__ __forceinline__ double exp2_series(double t) {
   t = fmax(t, -1200.0);
@@ -183,26 +207,32 @@ __device__ __forceinline__ double exp2_series(double t) {
 }
 // weight of the lower end of the bin that lies b bins (a whole number, any size) below the first
 __device__ __forceinline__ double bin_weight(float b, const Settings& set) { return exp2_series(-(double)b * set.bin_log2); }
-// (below the 1024 bins: e^-16 and less at temperatures up to two, which an fp32 exponential does)
-__device__ __forceinline__ double rest_weight(float b, const Settings& set) {
-  return set.temperature <= 2.f ? (double)__builtin_amdgcn_exp2f(fmaxf((float)set.bin_log2 * -b, -1200.f)) : bin_weight(b, set);
-}
+// Below the 1024 bins a weight is e^-16 and less at temperatures up to two, and all of a row's together 0.06 of the row's at most (2^19 tokens): an
+// fp32 exponential of the whole argument does, good to 2^-18.
+__device__ __forceinline__ bool rest_is_small(const Settings& set) { return set.temperature <= 2.f; }
+__device__ __forceinline__ float small_rest(float b, float place, float bin_log2) { return __builtin_amdgcn_exp2f(bin_log2 * (place - b)); }
 constexpr double kPlaceToRow = (double)(1u << (kFraction - kPlaceBits));
 
 // All weights of a row, relative to the bin of its maximum: table[b] = bin_weight(b) 2^(kFraction - kPlaceBits)
 struct Weights {
   const double* table;
-  float first, z;
+  float first;
+  PlaceExcess excess;
   __device__ __forceinline__ Weights(const Settings& set, float top, const double* t)
-      : table(t), first(set.bin_of(top)), z(place_factor(set)) {}
+      : table(t), first(set.bin_of(top)), excess(set, kPlaceOne) {}
   static __device__ __forceinline__ void fill(const Settings& set, double* table) {
     for (int b = threadIdx.x; b < kBins; b += blockDim.x) table[b] = bin_weight((float)b, set) * kPlaceToRow;
   }
   __device__ __forceinline__ uint64_t operator()(const Settings& set, float x) const {
+    if (x == -INFINITY) return 0;
     float place;
     const float b = first - set.bin_of(x, place);
     constexpr double kShift = 4503599627370496.0;        // 2^52: the sum's low bits are the rounded whole number
-    const double w = (b < (float)kBins ? table[(int)b] : rest_weight(b, set) * kPlaceToRow) * (double)place_weight(place, z) + kShift;
+    double w;
+    if (b < (float)kBins) w = table[(int)b] * (double)place_weight(place, excess);
+    else if (rest_is_small(set)) w = (double)small_rest(b, place, (float)set.bin_log2) * (double)(1ull << kFraction);
+    else w = bin_weight(b, set) * kPlaceToRow * (double)place_weight(place, excess);
+    w += kShift;
     return __builtin_bit_cast(uint64_t, w) - __builtin_bit_cast(uint64_t, kShift);
   }
 };
@@ -307,8 +337,7 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int v0 = s * p.slice, end = min(v0 + p.slice, p.V);
   float4 f[EPT / 4];
-#pragma unroll
-  for (int i = 0; i < EPT / 4; ++i) f[i] = logits4(x, v0 + 4 * (i * kThreads + tid), end);
+  read_logits<EPT / 4, kThreads, Number>(x, v0, tid, end, f);
   const Settings set(p, r);
   const bool filtered = set.filtered();
   unsigned long long* const bins = reinterpret_cast<unsigned long long*>(shared);
@@ -319,12 +348,14 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < EPT / 4; ++i) top = fmaxf(top, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
-  top = block_max(top, shf);
-  const float first = set.bin_of(top), z = place_factor(set);
+  top = fminf(block_max(top, shf), 3.402823466e38f);
+  const float first = set.bin_of(top), bin_log2 = (float)set.bin_log2;
   double total = 0.0;
-  uint32_t n = 0;
+  float rest = 0.f;
+  uint32_t n = 0;            // of the wavefront
   if (top > -INFINITY) {
     if (filtered) {
+      const PlaceExcess excess(set, kPlaceOne);
 #pragma unroll
       for (int i = 0; i < EPT / 4; ++i)
 #pragma unroll
@@ -332,11 +363,13 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
           const float l = get(f[i], e);
           float place;
           const float b = first - set.bin_of(l, place);
-          n += l > -INFINITY;
-          if (b < (float)kBins) atomicAdd(&bins[(int)b], 1ull << kCountAt | place_weight(place, z));
-          else if (l > -INFINITY) total += rest_weight(b, set) * (1.0 + place_excess(place, z));
+          const bool is = l > -INFINITY;                 // (in a row of masks of the type's lowest value such a logit would be in bin 0)
+          n += (uint32_t)__popcll(__ballot(is));
+          if (is && b < (float)kBins) atomicAdd(&bins[(int)b], 1ull << kCountAt | place_weight(place, excess));
+          if (is && b >= (float)kBins) rest += small_rest(b, place, bin_log2);
         }
     } else {
+      const PlaceExcess excess(set);
 #pragma unroll
       for (int i = 0; i < EPT / 4; ++i)
 #pragma unroll
@@ -344,11 +377,22 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
           const float l = get(f[i], e);
           float place;
           const float b = first - set.bin_of(l, place);
-          const double q = 1.0 + place_excess(place, z);
-          if (b < (float)kBins) total += table[(int)b] * q;
-          else if (l > -INFINITY) total += rest_weight(b, set) * q;
+          const bool is = l > -INFINITY;
+          if (is && b < (float)kBins) total = __builtin_fma(table[(int)b], 1.0 + (double)excess(place), total);
+          if (is && b >= (float)kBins) rest += small_rest(b, place, bin_log2);
         }
     }
+    if (!rest_is_small(set)) {                           // the same in 64 bits, from the logits once more
+      const PlaceExcess excess(set);
+      rest = 0.f;
+      for (int v = v0 + tid; v < end; v += kThreads) {
+        const float l = number(load1(x + v));
+        float place;
+        const float b = first - set.bin_of(l, place);
+        if (l > -INFINITY && b >= (float)kBins) total += bin_weight(b, set) * (1.0 + (double)excess(place));
+      }
+    }
+    total += (double)rest;
   }
   const int64_t at = (int64_t)r * p.slices + s;
   if (filtered) {
@@ -356,8 +400,6 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
     const uint64_t word = bins[tid];
     p.bins[at * kBins + tid] = word;
     total += (double)(word & kWeightMask) * (1.0 / (double)(1u << kPlaceBits)) * bin_weight((float)tid, set);
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) n += __shfl_xor(n, d, 64);
     if ((tid & 63) == 0) atomicAdd(&all, n);
   }
   total = block_sum(total, shd);
@@ -371,6 +413,7 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) 
 // ---- gather ----------------------------------------------------------------------------------------
 
 constexpr int kMostSlices = 128;
+constexpr int kReadAhead = 4;                            // loads of a thread on their way
 
 // Bins from the row's first down to the slice's first; kBins: none of the slice's is among the row's.
 __device__ __forceinline__ int shift_of(const Settings& set, float top, float row_top) {
@@ -385,7 +428,7 @@ __device__ __forceinline__ uint64_t total_of(const SliceStats& st, const Setting
 // grid: (slices, rows)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p) {
-  __shared__ uint64_t sh[4 * kWaves];
+  __shared__ uint64_t sh[3 * kWaves];
   __shared__ int shift[kMostSlices];
   __shared__ float shf[kWaves];
   __shared__ int k_bin, p_bin;
@@ -411,21 +454,31 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
   if (tid < p.slices) shift[tid] = shift_of(set, st.top, top);
   __syncthreads();
   // thread b: bin b of the row (what slices hold further down is in none of them)
-  uint64_t mine = 0, m = 0, n = 0;
-#pragma unroll 4
-  for (int i = 0; i < p.slices; ++i) {
-    const int b = tid - shift[i];
-    const uint64_t w = b >= 0 ? p.bins[(row + i) * kBins + b] : 0;
-    n += w >> kCountAt;
-    m += w & kWeightMask;
-    if (i == s) mine = w & kWeightMask;
+  uint64_t mine = 0, m = 0, n = 0, n_front = 0;            // mine: this slice's; n_front: of those in front of it
+  for (int i0 = 0; i0 < p.slices; i0 += 8) {
+    uint64_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = min(i0 + i, p.slices - 1), b = tid - shift[at];
+      w[i] = p.bins[(row + at) * kBins + max(b, 0)];
+      if (b < 0 || i0 + i >= p.slices) w[i] = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i == s) {
+        n_front = n;
+        mine = w[i];
+      }
+      n += w[i] >> kCountAt;
+      m += w[i] & kWeightMask;
+    }
   }
   const double to_row = bin_weight((float)tid, set) * kPlaceToRow;
   m = (uint64_t)((double)m * to_row);
-  uint64_t sums[4] = {n, m, whole, (uint64_t)(uint32_t)st.n}, totals[4];
-  block_scan64<4>(sums, totals, sh);
-  const uint64_t n_upto = sums[0], m_upto = sums[1];
-  const int k = (uint64_t)set.k < totals[3] ? set.k : 0;
+  uint64_t sums[3] = {n | (uint64_t)(uint32_t)st.n << 32, m, whole}, totals[3];
+  block_scan64<3>(sums, totals, sh);
+  const uint64_t n_upto = (uint32_t)sums[0], m_upto = sums[1];
+  const int k = (uint64_t)set.k < totals[0] >> 32 ? set.k : 0;
   if (k == 0 && set.top_p == 1.f && set.min_p == 0.f) {
     if (s == 0 && tid == 0) p.plan[r] = RowPlan{top, kEverything, 0, 0, 0, 0};
     if (tid == s) p.stats[row + s].above = whole;
@@ -457,14 +510,8 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
     p.plan[r] = RowPlan{top, slow ? kSlow : kFromList, (int)listed, k, limit, k > 0 ? 0 : above_m};
   if (slow) return;
   // this slice's tokens in the list's bins, those of the slices in front of it, and what it has above the list's bins
-  uint64_t parts[2] = {0, tid < lo ? (uint64_t)((double)mine * to_row) : 0}, of[2];
-  if (tid >= lo && tid <= hi)
-    for (int i = 0; i <= s; ++i) {
-      const int b = tid - shift[i];
-      if (b < 0) continue;
-      const uint64_t c = p.bins[(row + i) * kBins + b] >> kCountAt;
-      parts[0] += i == s ? c << 32 : c;
-    }
+  const bool among = tid >= lo && tid <= hi;
+  uint64_t parts[2] = {among ? (mine >> kCountAt) << 32 | n_front : 0, tid < lo ? (uint64_t)((double)(mine & kWeightMask) * to_row) : 0}, of[2];
   block_scan64<2>(parts, of, sh);
   if (tid == 0) p.stats[row + s].above = of[1];
   if ((of[0] >> 32) == 0) return;
@@ -472,18 +519,23 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p)
   const uint32_t list_at = (uint32_t)of[0];              // (the slice adds as many as the histogram says)
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int end = min((s + 1) * p.slice, p.V);
-  const float first = set.bin_of(top);
-#pragma unroll 4
-  for (int v = s * p.slice + 4 * tid; v < end; v += 4 * kThreads) {
-    const float4 f = logits4(x, v, end);
+  // the list's bins as logits, least <= l < past (exact: a bin's lower end times a power of two, or the next number above)
+  const double first = (double)set.bin_of(top);
+  const float least = first - hi <= -(double)kFar ? -3.402823466e38f : at_least((first - hi) / (double)set.per_bin);
+  const float past = first - lo + 1 >= (double)kFar ? INFINITY : at_least((first - lo + 1) / (double)set.per_bin);
+  for (int v0 = s * p.slice; v0 < end; v0 += 4 * kReadAhead * kThreads) {
+    float4 f[kReadAhead];
+    read_logits<kReadAhead, kThreads>(x, v0, tid, end, f);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float l = get(f, e), b = first - set.bin_of(l);
-      if (l > -INFINITY && b >= (float)lo && b <= (float)hi) {
-        const uint32_t to = list_at + atomicAdd(&used, 1u);
-        if (to < kList) list[to] = ((uint64_t)~score_key(l) << 32) | (uint32_t)(v + e);
+    for (int i = 0; i < kReadAhead; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float l = get(f[i], e);
+        if (l >= least && l < past) {
+          const uint32_t to = list_at + atomicAdd(&used, 1u);
+          if (to < kList) list[to] = ((uint64_t)~score_key(l) << 32) | (uint32_t)(v0 + 4 * (i * kThreads + tid) + e);
+        }
       }
-    }
   }
 }
 
@@ -585,7 +637,27 @@ __device__ void slow_border(const T* x, int V, const Settings& set, int k, float
   __syncthreads();
 }
 
-// Ascending.  Up to 256: every element's place is the number of those below it, counted by four threads each.  More: a bitonic network.
+// One step of a bitonic network among a wavefront's lanes, and all steps from STEP down.
+template <int STEP>
+__device__ __forceinline__ uint64_t other_lane64(uint64_t x) {
+  if constexpr (STEP == 1) return lane_move64<0xb1, 0xf, true>(x);                                    // quad_perm 1 0 3 2
+  if constexpr (STEP == 2) return lane_move64<0x4e, 0xf, true>(x);                                    // quad_perm 2 3 0 1
+  if constexpr (STEP == 4) return lane_move64<0x141, 0xf, true>(lane_move64<0x1b, 0xf, true>(x));     // a quad's, then eight lanes' order turned round
+  if constexpr (STEP == 8) return lane_move64<0x128, 0xf, true>(x);                                   // row_ror:8
+  return (uint64_t)__shfl_xor((unsigned long long)x, STEP, 64);
+}
+template <int STEP>
+__device__ __forceinline__ void sort_step(uint64_t& x, int lane, bool up) {
+  const uint64_t y = other_lane64<STEP>(x);
+  if ((y < x) == (((lane & STEP) == 0) == up)) x = y;
+}
+template <int STEP>
+__device__ __forceinline__ void sort_half(uint64_t& x, int lane, bool up) {
+  sort_step<STEP>(x, lane, up);
+  if constexpr (STEP > 1) sort_half<STEP / 2>(x, lane, up);
+}
+// Ascending.  Up to 256: every element's place is the number of those below it, counted by four threads each.  More: a bitonic network, whose
+// steps of less than 64 are done in registers.
 constexpr int kRanked = 256;
 __device__ __forceinline__ void sort_list(uint64_t* list, int n, uint64_t* spare, uint32_t* rank) {
   const int tid = threadIdx.x;
@@ -611,8 +683,20 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n, uint64_t* spare
   while (n2 < n) n2 *= 2;
   for (int i = n + tid; i < n2; i += kThreads) list[i] = ~0ull;
   __syncthreads();
-  for (int size = 2; size <= n2; size *= 2)
-    for (int step = size / 2; step > 0; step /= 2) {
+  const int lane = tid & 63, wave = tid >> 6;
+  for (int g = wave; g < n2 / 64; g += kWaves) {
+    uint64_t x = list[64 * g + lane];
+    sort_step<1>(x, lane, (lane & 2) == 0);
+    sort_step<2>(x, lane, (lane & 4) == 0), sort_step<1>(x, lane, (lane & 4) == 0);
+    sort_step<4>(x, lane, (lane & 8) == 0), sort_step<2>(x, lane, (lane & 8) == 0), sort_step<1>(x, lane, (lane & 8) == 0);
+    sort_step<8>(x, lane, (lane & 16) == 0), sort_half<4>(x, lane, (lane & 16) == 0);
+    sort_step<16>(x, lane, (lane & 32) == 0), sort_half<8>(x, lane, (lane & 32) == 0);
+    sort_half<32>(x, lane, (g & 1) == 0);
+    list[64 * g + lane] = x;
+  }
+  __syncthreads();
+  for (int size = 128; size <= n2; size *= 2) {
+    for (int step = size / 2; step >= 64; step /= 2) {
       for (int i = tid; i < n2 / 2; i += kThreads) {
         const int a = 2 * i - (i & (step - 1)), b = a + step;
         const uint64_t xa = list[a], xb = list[b];
@@ -623,6 +707,13 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n, uint64_t* spare
       }
       __syncthreads();
     }
+    for (int g = wave; g < n2 / 64; g += kWaves) {
+      uint64_t x = list[64 * g + lane];
+      sort_half<32>(x, lane, (64 * g & size) == 0);
+      list[64 * g + lane] = x;
+    }
+    __syncthreads();
+  }
 }
 __device__ __forceinline__ uint32_t listed_key(uint64_t x) { return ~(uint32_t)(x >> 32); }
 
@@ -720,8 +811,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
   // the token: the wavefronts take consecutive shares of the slice
   const int s = at_slice, end = min((s + 1) * p.slice, p.V), share = p.slice / kWaves, v0 = s * p.slice + wave * share;
   const int v1 = min(v0 + share, end);
-  const auto kept_weights = [&](int v, uint64_t (&w)[4]) {
-    const float4 f = logits4(x, v, end);
+  const auto kept_weights = [&](const float4& f, int v, uint64_t (&w)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float l = get(f, e);
@@ -730,11 +820,15 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
     }
   };
   uint64_t sum = 0;
-#pragma unroll 4
-  for (int v = v0 + 4 * lane; v < v1; v += 256) {
-    uint64_t w[4];
-    kept_weights(v, w);
-    sum += (w[0] + w[1]) + (w[2] + w[3]);
+  for (int v = v0; v < v1; v += 256 * kReadAhead) {
+    float4 f[kReadAhead];
+    read_logits<kReadAhead, 64>(x, v, lane, v1, f);
+#pragma unroll
+    for (int i = 0; i < kReadAhead; ++i) {
+      uint64_t w[4];
+      kept_weights(f[i], v + 4 * (i * 64 + lane), w);
+      sum += (w[0] + w[1]) + (w[2] + w[3]);
+    }
   }
   sum = wave_sum64(sum);
   if (lane == 0) sh[wave] = sum;
@@ -746,8 +840,10 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
   if (in_all == 0 && tid == 0) p.tokens[r] = index < p.V ? index : s * p.slice;
   if (run > target || run + sum <= target) return;
   for (int v = v0 + 4 * lane; v - 4 * lane < v1; v += 256) {
-    uint64_t w[4] = {0, 0, 0, 0};
-    if (v < v1) kept_weights(v, w);
+    float4 f[1];
+    read_logits<1, 64>(x, v - 4 * lane, lane, v1, f);
+    uint64_t w[4];
+    kept_weights(f[0], v, w);
     const uint64_t mine = (w[0] + w[1]) + (w[2] + w[3]), upto = run + wave_scan64(mine);
     const uint64_t hit = __ballot(upto > target);
     if (hit) {
@@ -775,32 +871,37 @@ __global__ __launch_bounds__(kThreads) void sample_probs_kernel(SampleParams p) 
   const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
   const Settings set(p, r);
   const Border border = p.border[r];
-  const float top = p.plan[r].top, first = set.bin_of(top), z = place_factor(set);
+  const float top = p.plan[r].top, first = set.bin_of(top);
+  const PlaceExcess excess(set);
   const double to_prob = border.inv_total * (double)(1ull << kFraction);
   table[tid] = (float)(bin_weight((float)tid, set) * to_prob);
   __syncthreads();
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   float* const out = p.probs + (int64_t)r * p.V;
   const int end = min((s + 1) * p.slice, p.V);
-#pragma unroll 4
-  for (int v = s * p.slice + 4 * tid; v < end; v += 4 * kThreads) {
-    const float4 f = logits4(x, v, end);
-    float4_u w;
+  for (int v0 = s * p.slice; v0 < end; v0 += 4 * kReadAhead * kThreads) {
+    float4 f[kReadAhead];
+    read_logits<kReadAhead, kThreads>(x, v0, tid, end, f);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float l = get(f, e);
-      const uint32_t kf = score_key(l);
-      w[e] = 0.f;
-      if (l > -INFINITY && (kf > border.key || (kf == border.key && v + e <= border.index))) {
-        float place;
-        const float b = first - set.bin_of(l, place), g = b < (float)kBins ? table[(int)b] : (float)(bin_weight(b, set) * to_prob);
-        w[e] = __builtin_fmaf(g, place_excess(place, z), g);
+    for (int i = 0; i < kReadAhead; ++i) {
+      const int v = v0 + 4 * (i * kThreads + tid);
+      float4_u w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float l = get(f[i], e);
+        const uint32_t kf = score_key(l);
+        w[e] = 0.f;
+        if (l > -INFINITY && (kf > border.key || (kf == border.key && v + e <= border.index))) {
+          float place;
+          const float b = first - set.bin_of(l, place), g = b < (float)kBins ? table[(int)b] : (float)(bin_weight(b, set) * to_prob);
+          w[e] = __builtin_fmaf(g, excess(place), g);
+        }
       }
-    }
-    if (v + 3 < end) {
-      *reinterpret_cast<float4_u*>(out + v) = w;
-    } else {
-      for (int e = 0; v + e < end; ++e) out[v + e] = w[e];
+      if (v + 3 < end) {
+        *reinterpret_cast<float4_u*>(out + v) = w;
+      } else {
+        for (int e = 0; v + e < end; ++e) out[v + e] = w[e];
+      }
     }
   }
 }

@@ -125,6 +125,17 @@ def test_masked_tokens_and_rows_of_nothing():
         assert tokens[1] == 2999 and tokens[2] == -1 and tokens[5] == -1 and tokens[4] in (5, 2000)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [70, 9000])
+def test_rows_of_the_lowest_value_and_nothing(dtype, V):
+    # masks of the type's lowest value weigh as any logit does where a row has nothing above them, those of -inf never
+    inf = float("inf")
+    lg = torch.full((6, V), -inf, dtype=dtype)
+    lg[:, 5:60:3] = torch.finfo(dtype).min
+    check(lg, torch.tensor([0.0, 0.3, 0.6, 0.99, 0.5, 0.5]), temperature=torch.tensor([1.0, 1.0, 0.7, 1.0, 3.0, 3.0]),
+          top_k=torch.tensor([0, 7, 0, 0, 0, 7], dtype=torch.int32), top_p=torch.tensor([1.0, 1.0, 0.5, 0.9, 1.0, 0.4]))
+
+
 def test_extreme_settings():
     lg, u = rows(8, 2000, seed=4)
     check(lg, u, temperature=[1e-30, 1e-4, 1e4, 3e38, float("inf"), 1.0, 1.0, 1.0], top_k=[0, 0, 0, 0, 0, -3, 1999, 2 ** 31 - 1])
