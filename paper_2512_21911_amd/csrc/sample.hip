@@ -36,7 +36,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kFraction = 43;                            // bits of a weight behind the point; 2^19 weights of 1.05 fit 63 bits
 constexpr int kPlaceBits = 31;                           // of a weight relative to its bin's: at least one, below two
-constexpr int kCountAt = 47;                             // a histogram's word: 2^15 such weights, and above them how many
+constexpr int kCountAt = 47;                             // a histogram's word: what 2^15 such weights have over one, and above that how many
 constexpr int kBins = 1024;                              // the last: everything below the others
 constexpr int kList = 4096;                              // tokens around the border that are sorted
 constexpr float kFar = 3e38f;                            // bins of logits further from zero are this one
@@ -45,7 +45,7 @@ constexpr double kLog2e = 1.4426950408889634074;
 struct SliceStats {
   float top;                 // largest logit; -inf: the slice has none above that
   int32_t n;                 // logits above -inf (rows with a filter)
-  double total;              // weight of all of them, relative to the bin of top
+  uint64_t total;            // weight of all of them, relative to the bin of top
   uint64_t above;            // weight that the slice keeps without those in the list, relative to the row's first bin
 };
 enum { kEverything, kFromList, kSlow };                  // how the border is found
@@ -54,7 +54,16 @@ struct RowPlan {
   int32_t how, listed, k;    // k: top-k, 0 if it drops nothing
   uint64_t limit, above;     // without top-k: the weight that the kept tokens reach, and what is above the list's bin
 };
-struct Border { uint32_t key; int32_t index; double inv_total; };     // inv_total: 1 / total weight of the kept tokens
+struct Border {              // of what a row keeps: logits above `least`, and those with it up to `index`
+  float least;
+  int32_t index;
+  double inv_total;          // 1 / their total weight
+  // (NaN is kept by no comparison; +inf is the largest finite number)
+  __device__ __forceinline__ bool keeps(float& l, int v) const {
+    l = l > 3.402823466e38f ? 3.402823466e38f : l;
+    return l > least || (l == least && v <= index);
+  }
+};
 
 struct SampleParams {
   const void* logits;
@@ -68,7 +77,7 @@ struct SampleParams {
   float* probs;
   int32_t rows, V, slice, slices;
   SliceStats* stats;         // [rows][slices]
-  uint64_t* bins;            // [rows][slices][kBins]: count << kCountAt | weight relative to the bin's
+  uint64_t* bins;            // [rows][slices][kBins]: count << kCountAt | what the weights, relative to the bin's, have over one
   uint64_t* list;            // [rows][kList]: ~key in the high half, index in the low one
   RowPlan* plan;             // [rows]
   Border* border;            // [rows]
@@ -93,8 +102,6 @@ __device__ __forceinline__ float4 load4(const __hip_bfloat16* p) {
 }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __hip_bfloat16* p) { return __bfloat162float(*p); }
-// (NaN alone; no more than a maximum takes)
-__device__ __forceinline__ float number(float x) { return fmaxf(x, -INFINITY); }
 // tokens v .. v + 3, -inf past the end
 template <typename T>
 __device__ __forceinline__ float4 logits4(const T* x, int v, int end) {
@@ -105,11 +112,9 @@ __device__ __forceinline__ float4 logits4(const T* x, int v, int end) {
   if (v + 3 < end) f.w = load1(x + v + 3);
   return f;
 }
-struct Clean { __device__ __forceinline__ float operator()(float x) const { return clean(x); } };
-struct Number { __device__ __forceinline__ float operator()(float x) const { return number(x); } };
 // Tokens v0 + 4 (i THREADS + thread) .. + 3 of all i < N.  Whether all threads' are inside the row is the same for the workgroup, and then the
 // loads are under no mask: under one they wait for each other (16.9 us instead of 13.x for the first launch at 64 rows of 129 280).
-template <int N, int THREADS, typename Each = Clean, typename T>
+template <int N, int THREADS, typename T>
 __device__ __forceinline__ void read_logits(const T* x, int v0, int thread, int end, float4 (&f)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -117,11 +122,9 @@ __device__ __forceinline__ void read_logits(const T* x, int v0, int thread, int 
     if (v + 4 * THREADS <= end) f[i] = load4(x + v + 4 * thread);
     else f[i] = logits4(x, v + 4 * thread, end);
   }
-#pragma unroll
-  for (int i = 0; i < N; ++i) f[i] = make_float4(Each()(f[i].x), Each()(f[i].y), Each()(f[i].z), Each()(f[i].w));
 }
-__device__ __forceinline__ float get(const float4& f, int i) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float get(const float4& f, int i) { return i == 0 ? f.x : i == 1 ? f.y : i == 2 ? f.z : f.w; }
 
 // the smallest fp32 number that is no less
 __device__ __forceinline__ float at_least(double x) {
@@ -174,17 +177,17 @@ struct Settings {
 
 // ---- weights ---------------------------------------------------------------------------------------
 
-// 2^(place bin_log2) - 1 times `scale`: four terms of the series, z = bin_log2 ln 2 <= 1/32
+// 2^(place bin_log2) - 1 times `scale`: x + x^2/2 + x^3/6 + x^4/24, x = place z, z = bin_log2 ln 2 <= 1/32, with the last term, on 0 <= place < 1, by
+// the cubic that Chebyshev's polynomial of degree four leaves (without its constant: no excess at place 0), 2^-30 of the weight at most.
 struct PlaceExcess {
-  float c1, c2, c3, c4;
+  float c1, c2, c3;
   __device__ __forceinline__ explicit PlaceExcess(const Settings& set, float scale = 1.f) {
-    const float z = (float)(set.bin_log2 * 0.69314718055994530942);
-    c1 = z * scale;
-    c2 = c1 * z * 0.5f;
-    c3 = c2 * z * (1.f / 3.f);
-    c4 = c3 * z * 0.25f;
+    const float z = (float)(set.bin_log2 * 0.69314718055994530942), x1 = z * scale, x2 = x1 * z * 0.5f, x3 = x2 * z * (1.f / 3.f), x4 = x3 * z * 0.25f;
+    c1 = x1 + 0.25f * x4;
+    c2 = x2 - 1.25f * x4;
+    c3 = x3 + 2.f * x4;
   }
-  __device__ __forceinline__ float operator()(float place) const { return place * (c1 + place * (c2 + place * (c3 + place * c4))); }
+  __device__ __forceinline__ float operator()(float place) const { return place * (c1 + place * (c2 + place * c3)); }
 };
 // 2^(place bin_log2) in fixed point; of an excess scaled by kPlaceOne
 constexpr float kPlaceOne = (float)(1u << kPlaceBits);
@@ -210,7 +213,7 @@ __device__ __forceinline__ double bin_weight(float b, const Settings& set) { ret
 // Below the 1024 bins a weight is e^-16 and less at temperatures up to two, and all of a row's together 0.06 of the row's at most (2^19 tokens): an
 // fp32 exponential of the whole argument does, good to 2^-18.
 __device__ __forceinline__ bool rest_is_small(const Settings& set) { return set.temperature <= 2.f; }
-__device__ __forceinline__ float small_rest(float b, float place, float bin_log2) { return __builtin_amdgcn_exp2f(bin_log2 * (place - b)); }
+__device__ __forceinline__ float small_rest(float below, float bin_log2) { return __builtin_amdgcn_exp2f(bin_log2 * -below); }
 constexpr double kPlaceToRow = (double)(1u << (kFraction - kPlaceBits));
 
 // All weights of a row, relative to the bin of its maximum: table[b] = bin_weight(b) 2^(kFraction - kPlaceBits)
@@ -220,19 +223,15 @@ struct Weights {
   PlaceExcess excess;
   __device__ __forceinline__ Weights(const Settings& set, float top, const double* t)
       : table(t), first(set.bin_of(top)), excess(set, kPlaceOne) {}
-  static __device__ __forceinline__ void fill(const Settings& set, double* table) {
-    for (int b = threadIdx.x; b < kBins; b += blockDim.x) table[b] = bin_weight((float)b, set) * kPlaceToRow;
-  }
   __device__ __forceinline__ uint64_t operator()(const Settings& set, float x) const {
     if (x == -INFINITY) return 0;
     float place;
     const float b = first - set.bin_of(x, place);
     constexpr double kShift = 4503599627370496.0;        // 2^52: the sum's low bits are the rounded whole number
     double w;
-    if (b < (float)kBins) w = table[(int)b] * (double)place_weight(place, excess);
-    else if (rest_is_small(set)) w = (double)small_rest(b, place, (float)set.bin_log2) * (double)(1ull << kFraction);
-    else w = bin_weight(b, set) * kPlaceToRow * (double)place_weight(place, excess);
-    w += kShift;
+    if (b < (float)kBins) w = __builtin_fma(table[(int)b], (double)place_weight(place, excess), kShift);
+    else if (rest_is_small(set)) w = __builtin_fma((double)small_rest(b - place, (float)set.bin_log2), (double)(1ull << kFraction), kShift);
+    else w = __builtin_fma(bin_weight(b, set) * kPlaceToRow, (double)place_weight(place, excess), kShift);
     return __builtin_bit_cast(uint64_t, w) - __builtin_bit_cast(uint64_t, kShift);
   }
 };
@@ -309,104 +308,119 @@ __device__ __forceinline__ float block_max(float x, float* sh) {
   __syncthreads();
   return x;
 }
-// (of a wavefront's lanes in a fixed order, then of the wavefronts')
-__device__ __forceinline__ double block_sum(double x, double* sh) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d, 64);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) x += sh[w];
-  __syncthreads();
-  return x;
-}
-
 // ---- stats -----------------------------------------------------------------------------------------
 
-constexpr uint64_t kWeightMask = (1ull << kCountAt) - 1;
+constexpr uint64_t kExcessMask = (1ull << kCountAt) - 1;
+__device__ __forceinline__ uint32_t count_of(uint64_t word) { return (uint32_t)(word >> kCountAt); }
+__device__ __forceinline__ uint64_t weight_of(uint64_t word) { return (word & kExcessMask) + ((uint64_t)count_of(word) << kPlaceBits); }
+
+struct StatsShared {
+  uint64_t bins[kBins];                                  // the histogram, or the bins' weights
+  float shf[kWaves];
+  uint64_t sums[2 * kWaves];
+};
+struct SliceFound {
+  float top;
+  uint64_t total;
+  uint32_t n;
+  uint64_t word;             // thread b: bin b
+};
+
+// By a workgroup, from its logits in registers (my_bin: bin_weight(thread); f: token 4 (i kThreads + thread) + e of x, which has n_x; NaN is among them still).
+template <typename T, int EPT>
+__device__ __forceinline__ SliceFound slice_stats(const Settings& set, double my_bin, const T* x, int n_x, const float4 (&f)[EPT / 4],
+                                                  StatsShared& sh) {
+  const int tid = threadIdx.x;
+  const bool filtered = set.filtered();
+  unsigned long long* const bins = reinterpret_cast<unsigned long long*>(sh.bins);
+  double* const table = reinterpret_cast<double*>(sh.bins);
+  if (filtered) bins[tid] = 0;
+  else table[tid] = my_bin;
+  SliceFound at;
+  at.top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < EPT / 4; ++i) at.top = fmaxf(at.top, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
+  at.top = fminf(block_max(at.top, sh.shf), 3.402823466e38f);
+  const float first = set.bin_of(at.top), bin_log2 = (float)set.bin_log2;
+  // Nearly always the bins' numbers are small, and no logit needs a bound: those of -inf and NaN are in no bin.
+  const bool near = fabsf(first) < 0x1p30f, small = rest_is_small(set);
+  double total = 0.0;
+  float rest = 0.f;
+  uint32_t n = 0;
+  if (near) {
+    const PlaceExcess excess(set, filtered ? kPlaceOne : 1.f);
+    const float first8 = 8.f * first;
+    const auto each = [&](auto&& in_bin) {
+#pragma unroll
+      for (int i = 0; i < EPT / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float l = get(f[i], e), bin = l * set.per_bin, b = floorf(bin), b8 = __builtin_fmaf(-8.f, b, first8);
+          if (b8 < 8.f * (float)kBins) {
+            in_bin((uint32_t)b8, excess(bin - b));
+          } else if (l > -INFINITY) {
+            rest += small_rest(first - bin, bin_log2);
+            ++n;
+          }
+        }
+    };
+    if (filtered) each([&](uint32_t b8, float y) { atomicAdd(reinterpret_cast<unsigned long long*>(reinterpret_cast<char*>(bins) + b8), 1ull << kCountAt | (uint32_t)y); });
+    else each([&](uint32_t b8, float y) { total = __builtin_fma(*reinterpret_cast<double*>(reinterpret_cast<char*>(table) + b8), 1.0 + (double)y, total); });
+    if (!small) rest = 0.f;
+  }
+  if (at.top > -INFINITY && !(near && small)) {            // the rest, or all, in 64 bits, from the logits once more
+    const PlaceExcess excess(set);
+    for (int v = tid; v < n_x; v += kThreads) {
+      const float l = clean(load1(x + v));
+      float place;
+      const float b = first - set.bin_of(l, place);
+      if (l == -INFINITY) continue;
+      if (b >= (float)kBins) {
+        total += bin_weight(b, set) * (1.0 + (double)excess(place));
+        if (!near) ++n;
+      } else if (!near) {
+        if (filtered) atomicAdd(&bins[(int)b], 1ull << kCountAt | (uint32_t)(excess(place) * kPlaceOne));
+        else total += table[(int)b] * (1.0 + (double)excess(place));
+      }
+    }
+  }
+  total += (double)rest;
+  at.word = 0;
+  if (filtered) {
+    __syncthreads();
+    at.word = bins[tid];
+    total += (double)weight_of(at.word) * (1.0 / (double)kPlaceOne) * my_bin;
+    n += count_of(at.word);
+  }
+  const uint64_t mine = wave_sum64((uint64_t)(total * (double)(1ull << kFraction))), count = wave_sum64(n);
+  const int lane = tid & 63;
+  if (lane == 63) {
+    sh.sums[tid >> 6] = mine;
+    sh.sums[kWaves + (tid >> 6)] = count;
+  }
+  __syncthreads();
+  at.total = wave_sum64(lane < kWaves ? sh.sums[lane] : 0);
+  at.n = (uint32_t)wave_sum64(lane < kWaves ? sh.sums[kWaves + lane] : 0);
+  return at;
+}
 
 // grid: (slices, rows).  EPT: logits of a thread, four at a time
 template <typename T, int EPT>
 __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleParams p) {
-  __shared__ uint64_t shared[kBins];                     // the histogram, or the bins' weights
-  __shared__ float shf[kWaves];
-  __shared__ double shd[kWaves];
-  __shared__ uint32_t all;
+  __shared__ StatsShared sh;
   const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int v0 = s * p.slice, end = min(v0 + p.slice, p.V);
   float4 f[EPT / 4];
-  read_logits<EPT / 4, kThreads, Number>(x, v0, tid, end, f);
+  read_logits<EPT / 4, kThreads>(x, v0, tid, end, f);
   const Settings set(p, r);
-  const bool filtered = set.filtered();
-  unsigned long long* const bins = reinterpret_cast<unsigned long long*>(shared);
-  double* const table = reinterpret_cast<double*>(shared);
-  if (filtered) bins[tid] = 0;
-  else table[tid] = bin_weight((float)tid, set);
-  if (tid == 0) all = 0;
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < EPT / 4; ++i) top = fmaxf(top, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
-  top = fminf(block_max(top, shf), 3.402823466e38f);
-  const float first = set.bin_of(top), bin_log2 = (float)set.bin_log2;
-  double total = 0.0;
-  float rest = 0.f;
-  uint32_t n = 0;            // of the wavefront
-  if (top > -INFINITY) {
-    if (filtered) {
-      const PlaceExcess excess(set, kPlaceOne);
-#pragma unroll
-      for (int i = 0; i < EPT / 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float l = get(f[i], e);
-          float place;
-          const float b = first - set.bin_of(l, place);
-          const bool is = l > -INFINITY;                 // (in a row of masks of the type's lowest value such a logit would be in bin 0)
-          n += (uint32_t)__popcll(__ballot(is));
-          if (is && b < (float)kBins) atomicAdd(&bins[(int)b], 1ull << kCountAt | place_weight(place, excess));
-          if (is && b >= (float)kBins) rest += small_rest(b, place, bin_log2);
-        }
-    } else {
-      const PlaceExcess excess(set);
-#pragma unroll
-      for (int i = 0; i < EPT / 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float l = get(f[i], e);
-          float place;
-          const float b = first - set.bin_of(l, place);
-          const bool is = l > -INFINITY;
-          if (is && b < (float)kBins) total = __builtin_fma(table[(int)b], 1.0 + (double)excess(place), total);
-          if (is && b >= (float)kBins) rest += small_rest(b, place, bin_log2);
-        }
-    }
-    if (!rest_is_small(set)) {                           // the same in 64 bits, from the logits once more
-      const PlaceExcess excess(set);
-      rest = 0.f;
-      for (int v = v0 + tid; v < end; v += kThreads) {
-        const float l = number(load1(x + v));
-        float place;
-        const float b = first - set.bin_of(l, place);
-        if (l > -INFINITY && b >= (float)kBins) total += bin_weight(b, set) * (1.0 + (double)excess(place));
-      }
-    }
-    total += (double)rest;
-  }
+  const SliceFound found = slice_stats<T, EPT>(set, bin_weight((float)tid, set), x + v0, end - v0, f, sh);
   const int64_t at = (int64_t)r * p.slices + s;
-  if (filtered) {
-    __syncthreads();
-    const uint64_t word = bins[tid];
-    p.bins[at * kBins + tid] = word;
-    total += (double)(word & kWeightMask) * (1.0 / (double)(1u << kPlaceBits)) * bin_weight((float)tid, set);
-    if ((tid & 63) == 0) atomicAdd(&all, n);
-  }
-  total = block_sum(total, shd);
+  if (set.filtered()) p.bins[at * kBins + tid] = found.word;
   if (tid == 0) {
-    p.stats[at].top = top;
-    p.stats[at].n = (int)all;
-    p.stats[at].total = total;
+    p.stats[at].top = found.top;
+    p.stats[at].n = (int)found.n;
+    p.stats[at].total = found.total;
   }
 }
 
@@ -422,120 +436,136 @@ __device__ __forceinline__ int shift_of(const Settings& set, float top, float ro
 // a slice's total relative to the row's first bin, in fixed point
 __device__ __forceinline__ uint64_t total_of(const SliceStats& st, const Settings& set, float row_top) {
   if (st.top == -INFINITY) return 0;
-  return (uint64_t)(st.total * bin_weight(set.bin_of(row_top) - set.bin_of(st.top), set) * (double)(1ull << kFraction));
+  return (uint64_t)((double)st.total * bin_weight(set.bin_of(row_top) - set.bin_of(st.top), set));
 }
+
+struct GatherShared {
+  uint64_t scan[2 * kWaves];
+  int bin;
+  uint64_t listed, above;
+  uint32_t used;
+  __device__ __forceinline__ void clear() {
+    bin = kBins;
+    used = 0;
+    listed = above = 0;
+  }
+};
+struct Bins { int lo, hi; };                             // those whose tokens are in the list
+
+// By a workgroup, thread b having bin b of the row (n tokens of weight m).  whole, count: the row's weight and its number of logits above -inf.
+// sh: cleared, a barrier ago.
+__device__ __forceinline__ RowPlan plan_row(const Settings& set, float top, uint64_t n, uint64_t m, uint64_t whole, uint32_t count,
+                                            GatherShared& sh, Bins& list) {
+  const int tid = threadIdx.x;
+  const int k = (uint32_t)set.k < count ? set.k : 0;
+  if (k == 0 && set.top_p == 1.f && set.min_p == 0.f) return RowPlan{top, kEverything, 0, 0, 0, 0};
+  const uint64_t limit = limit_of(set.top_p, whole), x = k > 0 ? n : m, wanted = k > 0 ? (uint64_t)k : limit;
+  uint64_t all;
+  const uint64_t upto = block_scan64(x, sh.scan, all);
+  if ((k > 0 || set.top_p < 1.f) && upto >= wanted && upto - x < wanted) sh.bin = tid;
+  __syncthreads();
+  // the border's bin; kBins: below them all
+  list.hi = sh.bin;
+  if (k == 0 && set.min_p > 0.f) {
+    const int m_bin = (int)fminf(set.bin_of(top) - set.bin_of(key_logit(set.least_key(top))), (float)kBins);
+    list.hi = min(list.hi, m_bin);
+  }
+  list.lo = k > 0 ? 0 : list.hi;
+  if (tid == list.hi) {
+    sh.listed = k > 0 ? upto : n;
+    sh.above = k > 0 ? 0 : upto - x;
+  }
+  __syncthreads();
+  const bool slow = list.hi == kBins || sh.listed > kList;
+  return RowPlan{top, slow ? kSlow : kFromList, (int)sh.listed, k, limit, sh.above};
+}
+
+// The list's bins as logits, least <= l <= most; both are exact, a bin's end times a power of two or the next number inwards.
+struct ListRange {
+  float least, most;
+  __device__ __forceinline__ ListRange(const Settings& set, float top, Bins list) {
+    const double first = (double)set.bin_of(top), lower = first - list.hi, past = first - list.lo + 1;
+    least = lower <= -(double)kFar ? -3.402823466e38f : at_least(lower / (double)set.per_bin);
+    most = past >= (double)kFar ? INFINITY : nextafterf(at_least(past / (double)set.per_bin), -INFINITY);
+  }
+  __device__ __forceinline__ bool has(float l) const { return l >= least && l <= most; }           // (never NaN)
+};
+__device__ __forceinline__ uint64_t listed(float l, int v) { return (uint64_t)~score_key(clean(l)) << 32 | (uint32_t)v; }
 
 // grid: (slices, rows)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleParams p) {
-  __shared__ uint64_t sh[3 * kWaves];
-  __shared__ int shift[kMostSlices];
-  __shared__ float shf[kWaves];
-  __shared__ int k_bin, p_bin;
-  __shared__ uint64_t upto_n, bin_n, above_m;
-  __shared__ uint32_t used;
-  const int tid = threadIdx.x, s = blockIdx.x, r = blockIdx.y;
+  __shared__ GatherShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, s = blockIdx.x, r = blockIdx.y;
   const int64_t row = (int64_t)r * p.slices;
-  SliceStats st{-INFINITY, 0, 0.0, 0};
-  if (tid < p.slices) st = p.stats[row + tid];
+  // every wavefront by itself: lane l has slices l and l + 64
+  SliceStats st[2] = {{-INFINITY, 0, 0, 0}, {-INFINITY, 0, 0, 0}};
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (lane + 64 * i < p.slices) st[i] = p.stats[row + lane + 64 * i];
   const Settings set(p, r);
-  if (tid == 0) {
-    k_bin = p_bin = kBins;
-    used = 0;
-    upto_n = bin_n = above_m = 0;
-  }
-  const float top = block_max(st.top, shf);
-  const uint64_t whole = tid < p.slices && top > -INFINITY ? total_of(st, set, top) : 0;
+  if (tid == 0) sh.clear();
+  const float top = wave_max(fmaxf(st[0].top, st[1].top));
+  const uint64_t whole[2] = {total_of(st[0], set, top), total_of(st[1], set, top)};
+  const auto keeps_all = [&] {
+    if (tid == (s & 63)) p.stats[row + s].above = s < 64 ? whole[0] : whole[1];
+  };
   if (!set.filtered() || top == -INFINITY) {
     if (s == 0 && tid == 0) p.plan[r] = RowPlan{top, kEverything, 0, 0, 0, 0};
-    if (tid == s) p.stats[row + s].above = whole;
+    keeps_all();
     return;
   }
-  if (tid < p.slices) shift[tid] = shift_of(set, st.top, top);
-  __syncthreads();
+  const int shift[2] = {shift_of(set, st[0].top, top), shift_of(set, st[1].top, top)};
   // thread b: bin b of the row (what slices hold further down is in none of them)
   uint64_t mine = 0, m = 0, n = 0, n_front = 0;            // mine: this slice's; n_front: of those in front of it
-  for (int i0 = 0; i0 < p.slices; i0 += 8) {
-    uint64_t w[8];
+  for (int i0 = 0; i0 < p.slices; i0 += 4) {
+    uint64_t w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int at = min(i0 + i, p.slices - 1), b = tid - shift[at];
+    for (int i = 0; i < 4; ++i) {
+      const int at = min(i0 + i, p.slices - 1), b = tid - __builtin_amdgcn_readlane(at < 64 ? shift[0] : shift[1], at & 63);
       w[i] = p.bins[(row + at) * kBins + max(b, 0)];
       if (b < 0 || i0 + i >= p.slices) w[i] = 0;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if (i0 + i == s) {
         n_front = n;
         mine = w[i];
       }
-      n += w[i] >> kCountAt;
-      m += w[i] & kWeightMask;
+      n += count_of(w[i]);
+      m += w[i] & kExcessMask;
     }
   }
   const double to_row = bin_weight((float)tid, set) * kPlaceToRow;
-  m = (uint64_t)((double)m * to_row);
-  uint64_t sums[3] = {n | (uint64_t)(uint32_t)st.n << 32, m, whole}, totals[3];
-  block_scan64<3>(sums, totals, sh);
-  const uint64_t n_upto = (uint32_t)sums[0], m_upto = sums[1];
-  const int k = (uint64_t)set.k < totals[0] >> 32 ? set.k : 0;
-  if (k == 0 && set.top_p == 1.f && set.min_p == 0.f) {
-    if (s == 0 && tid == 0) p.plan[r] = RowPlan{top, kEverything, 0, 0, 0, 0};
-    if (tid == s) p.stats[row + s].above = whole;
-    return;
-  }
-  const uint64_t limit = limit_of(set.top_p, totals[2]);
-  if (k > 0) {
-    if (n_upto >= (uint64_t)k && n_upto - n < (uint64_t)k) k_bin = tid;
-  } else if (set.top_p < 1.f) {
-    if (m_upto >= limit && m_upto - m < limit) p_bin = tid;
-  }
+  m = (uint64_t)((double)(m + (n << kPlaceBits)) * to_row);
+  Bins bins;
   __syncthreads();
-  // the border's bin; kBins: below them all
-  int hi = k > 0 ? k_bin : p_bin;
-  if (k == 0 && set.min_p > 0.f) {
-    const int m_bin = (int)fminf(set.bin_of(top) - set.bin_of(key_logit(set.least_key(top))), (float)kBins);
-    hi = set.top_p < 1.f ? min(hi, m_bin) : m_bin;
-  }
-  const int lo = k > 0 ? 0 : hi;
-  if (tid == hi) {
-    upto_n = n_upto;
-    bin_n = n;
-    above_m = m_upto - m;
-  }
-  __syncthreads();
-  const uint64_t listed = k > 0 ? upto_n : bin_n;
-  const bool slow = hi == kBins || listed > kList;
-  if (s == 0 && tid == 0)
-    p.plan[r] = RowPlan{top, slow ? kSlow : kFromList, (int)listed, k, limit, k > 0 ? 0 : above_m};
-  if (slow) return;
+  const RowPlan plan = plan_row(set, top, n, m, wave_sum64(whole[0] + whole[1]), (uint32_t)wave_sum64((uint32_t)(st[0].n + st[1].n)), sh, bins);
+  if (s == 0 && tid == 0) p.plan[r] = plan;
+  if (plan.how == kEverything) keeps_all();
+  if (plan.how != kFromList) return;
   // this slice's tokens in the list's bins, those of the slices in front of it, and what it has above the list's bins
-  const bool among = tid >= lo && tid <= hi;
-  uint64_t parts[2] = {among ? (mine >> kCountAt) << 32 | n_front : 0, tid < lo ? (uint64_t)((double)(mine & kWeightMask) * to_row) : 0}, of[2];
-  block_scan64<2>(parts, of, sh);
+  const bool among = tid >= bins.lo && tid <= bins.hi;
+  uint64_t parts[2] = {among ? (uint64_t)count_of(mine) << 32 | n_front : 0, tid < bins.lo ? (uint64_t)((double)weight_of(mine) * to_row) : 0}, of[2];
+  block_scan64<2>(parts, of, sh.scan);
   if (tid == 0) p.stats[row + s].above = of[1];
   if ((of[0] >> 32) == 0) return;
   uint64_t* const list = p.list + (int64_t)r * kList;
   const uint32_t list_at = (uint32_t)of[0];              // (the slice adds as many as the histogram says)
   const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
   const int end = min((s + 1) * p.slice, p.V);
-  // the list's bins as logits, least <= l < past (exact: a bin's lower end times a power of two, or the next number above)
-  const double first = (double)set.bin_of(top);
-  const float least = first - hi <= -(double)kFar ? -3.402823466e38f : at_least((first - hi) / (double)set.per_bin);
-  const float past = first - lo + 1 >= (double)kFar ? INFINITY : at_least((first - lo + 1) / (double)set.per_bin);
+  const ListRange range(set, top, bins);
   for (int v0 = s * p.slice; v0 < end; v0 += 4 * kReadAhead * kThreads) {
     float4 f[kReadAhead];
     read_logits<kReadAhead, kThreads>(x, v0, tid, end, f);
 #pragma unroll
     for (int i = 0; i < kReadAhead; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float l = get(f[i], e);
-        if (l >= least && l < past) {
-          const uint32_t to = list_at + atomicAdd(&used, 1u);
-          if (to < kList) list[to] = ((uint64_t)~score_key(l) << 32) | (uint32_t)(v0 + 4 * (i * kThreads + tid) + e);
+      for (int e = 0; e < 4; ++e)
+        if (range.has(get(f[i], e))) {
+          const uint32_t to = list_at + atomicAdd(&sh.used, 1u);
+          if (to < kList) list[to] = listed(get(f[i], e), v0 + 4 * (i * kThreads + tid) + e);
         }
-      }
   }
 }
 
@@ -717,69 +747,62 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n, uint64_t* spare
 }
 __device__ __forceinline__ uint32_t listed_key(uint64_t x) { return ~(uint32_t)(x >> 32); }
 
-// grid: (rows)
+struct DrawShared {
+  uint64_t list[kList];
+  uint64_t spare[kRanked];
+  uint32_t rank[kRanked];
+  double table[kBins];
+  uint64_t scan[2 * kWaves];
+  unsigned long long kept[kMostSlices];                  // weight that a slice keeps
+  int at_slice;
+  uint64_t in_slice, in_row;                             // the target in front of which so much of the slice, of the row, is
+  uint32_t key;                                          // the border that the list gives
+  int index, stay;
+};
+
+// The border and the token of a row, by a workgroup.  sh.list: the listed tokens in any order; sh.kept: what slices keep without those.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
-  __shared__ uint64_t list[kList];
-  __shared__ uint64_t spare[kRanked];
-  __shared__ uint32_t rank[kRanked];
-  __shared__ double table[kBins];
-  __shared__ uint64_t sh[2 * kWaves];
-  __shared__ unsigned long long kept[kMostSlices];       // weight that a slice keeps
-  __shared__ int at_slice;
-  __shared__ uint64_t in_slice;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x;
-  const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
-  const RowPlan plan = p.plan[r];
-  const float top = plan.top;
-  if (top == -INFINITY) {
-    if (tid == 0) {
-      if (p.tokens) p.tokens[r] = -1;
-      p.border[r] = Border{0xffffffffu, -1, 0.0};
-    }
-    return;
-  }
-  if (tid < p.slices) kept[tid] = plan.how == kSlow ? 0 : p.stats[(int64_t)r * p.slices + tid].above;
-  if (plan.how == kFromList)
-    for (int i = tid; i < plan.listed; i += kThreads) list[i] = p.list[(int64_t)r * kList + i];
-  const Settings set(p, r);
-  Weights::fill(set, table);
-  const Weights weight(set, top, table);
+__device__ __forceinline__ void draw_row(const SampleParams& p, int r, const T* x, const Settings& set, double my_bin, const RowPlan& plan,
+                                         DrawShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  sh.table[tid] = my_bin * kPlaceToRow;
+  const Weights weight(set, plan.top, sh.table);
   __syncthreads();
   uint32_t key = 0;
   int index = p.V;
   if (plan.how == kFromList) {
-    const int n = plan.listed;
-    sort_list(list, n, spare, rank);
-    const int n_k = plan.k > 0 ? min(plan.k, n) : n;
-    uint64_t limit = plan.limit, all;
-    if (plan.k > 0 && set.top_p < 1.f) {
-      uint64_t w = 0;
-      for (int i = tid; i < n_k; i += kThreads) w += weight(set, key_logit(listed_key(list[i])));
-      block_scan64(w, sh, all);
-      limit = limit_of(set.top_p, all);
+    const uint32_t least = set.least_key(plan.top);
+    if (tid == 0) {
+      sh.key = least;
+      sh.index = p.V;
+      sh.stay = 0;
     }
-    const uint32_t least = set.least_key(top);
-    uint64_t before = plan.above, stay = 0;
-    for (int i0 = 0; i0 < n_k; i0 += kThreads) {
-      const int i = i0 + tid;
-      const uint32_t ki = i < n_k ? listed_key(list[i]) : 0;
-      const uint64_t w = i < n_k ? weight(set, key_logit(ki)) : 0;
-      const uint64_t upto = before + block_scan64(w, sh, all);
-      const bool stays = i < n_k && (set.top_p == 1.f || upto - w < limit) && ki >= least;
-      stay += stays;
-      before += all;
-      if (stays) atomicAdd(&kept[(int)(uint32_t)list[i] / p.slice], (unsigned long long)w);
+    sort_list(sh.list, plan.listed, sh.spare, sh.rank);
+    const int n = plan.k > 0 ? min(plan.k, plan.listed) : plan.listed;
+    const int each = (n + kThreads - 1) / kThreads, i0 = min(tid * each, n), i1 = min(i0 + each, n);
+    uint64_t sum = 0, all;
+    for (int i = i0; i < i1; ++i) sum += weight(set, key_logit(listed_key(sh.list[i])));
+    uint64_t upto = plan.above + block_scan64(sum, sh.scan, all) - sum;
+    const uint64_t limit = plan.k > 0 ? limit_of(set.top_p, all) : plan.limit;
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t ki = listed_key(sh.list[i]);
+      if ((set.top_p < 1.f && upto >= limit) || ki < least) break;
+      const uint64_t w = weight(set, key_logit(ki));
+      upto += w;
+      const int v = (int)(uint32_t)sh.list[i];
+      atomicAdd(&sh.kept[v / p.slice], (unsigned long long)w);
+      if (i < kRanked) sh.spare[i] = w;
+      if (i + 1 == n || (set.top_p < 1.f && upto >= limit) || listed_key(sh.list[i + 1]) < least) {
+        sh.key = ki;
+        sh.index = v;
+        sh.stay = i + 1;
+      }
     }
-    block_scan64(stay, sh, all);
-    if (all > 0) {
-      key = listed_key(list[all - 1]);
-      index = (int)(uint32_t)list[all - 1];
-    } else {
-      key = least;
-    }
+    __syncthreads();
+    key = sh.key;
+    index = sh.index;
   } else if (plan.how == kSlow) {
-    slow_border<T>(x, p.V, set, plan.k, top, weight, reinterpret_cast<unsigned long long*>(list), sh, key, index);
+    slow_border<T>(x, p.V, set, plan.k, plan.top, weight, reinterpret_cast<unsigned long long*>(sh.list), sh.scan, key, index);
     for (int s = 0; s < p.slices; ++s) {
       uint64_t w = 0, all;
       for (int v = s * p.slice + tid; v < min((s + 1) * p.slice, p.V); v += kThreads) {
@@ -787,79 +810,152 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
         const uint32_t kf = score_key(f);
         if (f > -INFINITY && (kf > key || (kf == key && v <= index))) w += weight(set, f);
       }
-      block_scan64(w, sh, all);
-      if (tid == 0) kept[s] = all;
+      block_scan64(w, sh.scan, all);
+      if (tid == 0) sh.kept[s] = all;
     }
   }
   __syncthreads();
+  Border border{key == 0 ? -INFINITY : key_logit(key), index, 0.0};
+  if (border.least == -INFINITY) border.index = -1;
   // the target, and the slice it falls in
   if (wave == 0) {
-    const uint64_t a = 2 * lane < p.slices ? kept[2 * lane] : 0, b = 2 * lane + 1 < p.slices ? kept[2 * lane + 1] : 0;
+    const uint64_t a = 2 * lane < p.slices ? sh.kept[2 * lane] : 0, b = 2 * lane + 1 < p.slices ? sh.kept[2 * lane + 1] : 0;
     const uint64_t upto = wave_scan64(a + b), total = lane64(upto, 63), front = upto - a - b;
     const double t = p.tokens ? (double)p.u[r] * (double)total : 0.0;
     uint64_t target = t > 0.0 ? (uint64_t)t : 0;
     target = min(target, total - 1);
     if (front <= target && target < upto) {
       const bool second = target >= front + a;
-      at_slice = 2 * lane + (second ? 1 : 0);
-      in_slice = target - front - (second ? a : 0);
+      sh.at_slice = 2 * lane + (second ? 1 : 0);
+      sh.in_slice = target - front - (second ? a : 0);
+      sh.in_row = target;
     }
-    if (lane == 0) p.border[r] = Border{key, index, 1.0 / (double)total};
+    if (lane == 0) p.border[r] = Border{border.least, border.index, 1.0 / (double)total};
   }
   if (!p.tokens) return;
   __syncthreads();
-  // the token: the wavefronts take consecutive shares of the slice
-  const int s = at_slice, end = min((s + 1) * p.slice, p.V), share = p.slice / kWaves, v0 = s * p.slice + wave * share;
-  const int v1 = min(v0 + share, end);
-  const auto kept_weights = [&](const float4& f, int v, uint64_t (&w)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float l = get(f, e);
-      const uint32_t kf = score_key(l);
-      w[e] = l > -INFINITY && (kf > key || (kf == key && v + e <= index)) ? weight(set, l) : 0;
+  if (plan.how == kFromList && plan.k > 0 && sh.stay <= kRanked) {       // all kept tokens are in the list: by what is in front of each, by index
+    uint64_t* const front = reinterpret_cast<uint64_t*>(sh.table);
+    const int n = sh.stay, i = tid & (kRanked - 1), part = tid / kRanked, each = (n + 3) / 4;
+    if (tid < kRanked) front[tid] = 0;
+    __syncthreads();
+    if (i < n) {
+      const uint32_t mine = (uint32_t)sh.list[i];
+      uint64_t sum = 0;
+      for (int j = part * each; j < min((part + 1) * each, n); ++j) sum += (uint32_t)sh.list[j] < mine ? sh.spare[j] : 0;
+      atomicAdd(reinterpret_cast<unsigned long long*>(&front[i]), (unsigned long long)sum);
     }
-  };
+    __syncthreads();
+    if (tid < n && front[tid] <= sh.in_row && sh.in_row < front[tid] + sh.spare[tid]) p.tokens[r] = (int)(uint32_t)sh.list[tid];
+    return;
+  }
+  // the token: the wavefronts take consecutive shares of the slice, then all of them the share that it is in
+  const int begin = sh.at_slice * p.slice, end = min(begin + p.slice, p.V), share = p.slice / kWaves;
+  const auto kept_weight = [&](float l, int v) -> uint64_t { return border.keeps(l, v) ? weight(set, l) : 0; };
   uint64_t sum = 0;
-  for (int v = v0; v < v1; v += 256 * kReadAhead) {
+  const int v1 = min(begin + (wave + 1) * share, end);
+  for (int v0 = begin + wave * share; v0 < v1; v0 += 256 * kReadAhead) {
     float4 f[kReadAhead];
-    read_logits<kReadAhead, 64>(x, v, lane, v1, f);
+    read_logits<kReadAhead, 64>(x, v0, lane, v1, f);
 #pragma unroll
-    for (int i = 0; i < kReadAhead; ++i) {
-      uint64_t w[4];
-      kept_weights(f[i], v + 4 * (i * 64 + lane), w);
-      sum += (w[0] + w[1]) + (w[2] + w[3]);
-    }
+    for (int i = 0; i < kReadAhead; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += kept_weight(get(f[i], e), v0 + 4 * (i * 64 + lane) + e);
   }
   sum = wave_sum64(sum);
-  if (lane == 0) sh[wave] = sum;
+  if (lane == 0) sh.scan[wave] = sum;
   __syncthreads();
-  const uint64_t upto_wave = wave_scan64(lane < kWaves ? sh[lane] : 0), in_all = lane64(upto_wave, kWaves - 1);
+  const uint64_t upto_wave = wave_scan64(lane < kWaves ? sh.scan[lane] : 0), in_all = lane64(upto_wave, kWaves - 1);
+  if (in_all == 0) {
+    if (tid == 0) p.tokens[r] = border.index >= 0 && border.index < p.V ? border.index : begin;
+    return;
+  }
   // (the bins' weights, rounded once each, may add up to a little more than the tokens': then it is the slice's last)
-  const uint64_t target = in_all > 0 ? min(in_slice, in_all - 1) : 0;
-  uint64_t run = lane64(upto_wave, __builtin_amdgcn_readfirstlane(wave)) - sum;
-  if (in_all == 0 && tid == 0) p.tokens[r] = index < p.V ? index : s * p.slice;
-  if (run > target || run + sum <= target) return;
-  for (int v = v0 + 4 * lane; v - 4 * lane < v1; v += 256) {
-    float4 f[1];
-    read_logits<1, 64>(x, v - 4 * lane, lane, v1, f);
-    uint64_t w[4];
-    kept_weights(f[0], v, w);
-    const uint64_t mine = (w[0] + w[1]) + (w[2] + w[3]), upto = run + wave_scan64(mine);
-    const uint64_t hit = __ballot(upto > target);
-    if (hit) {
-      if (lane == __builtin_ctzll(hit)) {
-        uint64_t c = upto - mine;
-        int e = 0;
-        for (; e < 3; ++e) {
-          c += w[e];
-          if (c > target) break;
-        }
-        p.tokens[r] = v + e;
-      }
+  const uint64_t target = min(sh.in_slice, in_all - 1);
+  const int at = __builtin_ctzll(__ballot(upto_wave > target));
+  const int each = (share + kThreads - 1) / kThreads, first = begin + at * share + tid * each, last = min(first + each, min(begin + (at + 1) * share, end));
+  uint64_t mine = 0, all;
+  for (int v = first; v < last; ++v) mine += kept_weight(load1(x + v), v);
+  __syncthreads();
+  uint64_t upto = (at > 0 ? lane64(upto_wave, at - 1) : 0) + block_scan64(mine, sh.scan, all);
+  if (upto <= target || upto - mine > target) return;
+  upto -= mine;
+  for (int v = first; v < last; ++v) {
+    upto += kept_weight(load1(x + v), v);
+    if (upto > target) {
+      p.tokens[r] = v;
       return;
     }
-    run = lane64(upto, 63);
   }
+}
+__device__ __forceinline__ void nothing_to_draw(const SampleParams& p, int r) {
+  if (threadIdx.x != 0) return;
+  if (p.tokens) p.tokens[r] = -1;
+  p.border[r] = Border{INFINITY, -1, 0.0};
+}
+
+// grid: (rows)
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p) {
+  __shared__ DrawShared sh;
+  const int tid = threadIdx.x, r = blockIdx.x;
+  const RowPlan plan = p.plan[r];
+  if (plan.top == -INFINITY) {
+    nothing_to_draw(p, r);
+    return;
+  }
+  if (tid < p.slices) sh.kept[tid] = plan.how == kSlow ? 0 : p.stats[(int64_t)r * p.slices + tid].above;
+  if (plan.how == kFromList)
+    for (int i = tid; i < plan.listed; i += kThreads) sh.list[i] = p.list[(int64_t)r * kList + i];
+  const Settings set(p, r);
+  draw_row<T>(p, r, static_cast<const T*>(p.logits) + (int64_t)r * p.stride, set, bin_weight((float)tid, set), plan, sh);
+}
+
+// ---- a row at a time -------------------------------------------------------------------------------
+
+// All of it for rows that a workgroup's registers hold.  grid: (rows)
+template <typename T, int EPT>
+__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleParams p) {
+  __shared__ StatsShared stats;
+  __shared__ GatherShared gather;
+  __shared__ DrawShared sh;
+  const int tid = threadIdx.x, r = blockIdx.x;
+  const T* const x = static_cast<const T*>(p.logits) + (int64_t)r * p.stride;
+  float4 f[EPT / 4];
+  read_logits<EPT / 4, kThreads>(x, 0, tid, p.V, f);
+  const Settings set(p, r);
+  const double my_bin = bin_weight((float)tid, set);
+  if (tid == 0) gather.clear();
+  const SliceFound found = slice_stats<T, EPT>(set, my_bin, x, p.V, f, stats);
+  if (found.top == -INFINITY) {
+    if (tid == 0 && p.probs) p.plan[r] = RowPlan{found.top, kEverything, 0, 0, 0, 0};
+    nothing_to_draw(p, r);
+    return;
+  }
+  RowPlan plan{found.top, kEverything, 0, 0, 0, 0};
+  uint64_t above = found.total;
+  if (set.filtered()) {
+    const uint64_t m = (uint64_t)((double)weight_of(found.word) * (my_bin * kPlaceToRow));
+    Bins bins;
+    plan = plan_row(set, found.top, count_of(found.word), m, found.total, found.n, gather, bins);
+    if (plan.how != kEverything) above = plan.how == kSlow ? 0 : plan.above;
+    if (plan.how == kFromList) {
+      const ListRange range(set, found.top, bins);
+#pragma unroll
+      for (int i = 0; i < EPT / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (range.has(get(f[i], e))) {
+            const uint32_t to = atomicAdd(&gather.used, 1u);
+            if (to < kList) sh.list[to] = listed(get(f[i], e), 4 * (i * kThreads + tid) + e);
+          }
+    }
+  }
+  if (tid == 0) {
+    sh.kept[0] = above;
+    if (p.probs) p.plan[r] = plan;
+  }
+  draw_row<T>(p, r, x, set, my_bin, plan, sh);
 }
 
 // ---- probabilities ---------------------------------------------------------------------------------
@@ -888,10 +984,9 @@ __global__ __launch_bounds__(kThreads) void sample_probs_kernel(SampleParams p) 
       float4_u w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float l = get(f[i], e);
-        const uint32_t kf = score_key(l);
+        float l = get(f[i], e);
         w[e] = 0.f;
-        if (l > -INFINITY && (kf > border.key || (kf == border.key && v + e <= border.index))) {
+        if (border.keeps(l, v + e)) {
           float place;
           const float b = first - set.bin_of(l, place), g = b < (float)kBins ? table[(int)b] : (float)(bin_weight(b, set) * to_prob);
           w[e] = __builtin_fmaf(g, excess(place), g);
@@ -910,7 +1005,7 @@ __global__ __launch_bounds__(kThreads) void sample_probs_kernel(SampleParams p) 
 
 // Tokens of a slice: as many workgroups as there are compute units, if the rows have that many slices of 4096.
 int slice_of(int rows, int V) {
-  const int wanted = std::max(1, 256 / rows), each = (V + wanted - 1) / wanted;
+  const int wanted = V <= 32768 ? 1 : std::max(1, 256 / rows), each = (V + wanted - 1) / wanted;
   int s = 4096;
   while (s < each && s < 32768) s *= 2;
   return s;
@@ -924,14 +1019,14 @@ struct Layout {
   Layout(int rows, int V) {
     slice = slice_of(rows, V);
     slices = (V + slice - 1) / slice;
-    const size_t n = (size_t)rows * slices;
+    const size_t n = slices > 1 ? (size_t)rows * slices : 0, lists = slices > 1 ? (size_t)rows : 0;       // (one: in its workgroup's LDS)
     size_t off = 0;
     stats = off;
     off += align256(n * sizeof(SliceStats));
     bins = off;
     off += align256(n * kBins * sizeof(uint64_t));
     list = off;
-    off += align256((size_t)rows * kList * sizeof(uint64_t));
+    off += align256(lists * kList * sizeof(uint64_t));
     plan = off;
     off += align256((size_t)rows * sizeof(RowPlan));
     border = off;
@@ -943,14 +1038,21 @@ struct Layout {
 template <typename T>
 hipError_t launch_sample(const SampleParams& p, hipStream_t st) {
   const dim3 grid((unsigned)p.slices, (unsigned)p.rows), block(kThreads);
+  const auto launch = [&](auto per_thread) {
+    constexpr int EPT = decltype(per_thread)::value;
+    if (p.slices == 1) hipLaunchKernelGGL((sample_row_kernel<T, EPT>), dim3((unsigned)p.rows), block, 0, st, p);
+    else hipLaunchKernelGGL((sample_stats_kernel<T, EPT>), grid, block, 0, st, p);
+  };
   switch (p.slice) {
-    case 4096: hipLaunchKernelGGL((sample_stats_kernel<T, 4>), grid, block, 0, st, p); break;
-    case 8192: hipLaunchKernelGGL((sample_stats_kernel<T, 8>), grid, block, 0, st, p); break;
-    case 16384: hipLaunchKernelGGL((sample_stats_kernel<T, 16>), grid, block, 0, st, p); break;
-    default: hipLaunchKernelGGL((sample_stats_kernel<T, 32>), grid, block, 0, st, p); break;
+    case 4096: launch(std::integral_constant<int, 4>()); break;
+    case 8192: launch(std::integral_constant<int, 8>()); break;
+    case 16384: launch(std::integral_constant<int, 16>()); break;
+    default: launch(std::integral_constant<int, 32>()); break;
   }
-  hipLaunchKernelGGL(sample_gather_kernel<T>, grid, block, 0, st, p);
-  hipLaunchKernelGGL(sample_draw_kernel<T>, dim3((unsigned)p.rows), block, 0, st, p);
+  if (p.slices > 1) {
+    hipLaunchKernelGGL(sample_gather_kernel<T>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(sample_draw_kernel<T>, dim3((unsigned)p.rows), block, 0, st, p);
+  }
   if (p.probs) hipLaunchKernelGGL(sample_probs_kernel<T>, grid, block, 0, st, p);
   return hipGetLastError();
 }
