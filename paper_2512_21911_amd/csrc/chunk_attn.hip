@@ -9,6 +9,7 @@ namespace {
 
 constexpr int kKeys = 64;                                // keys of a unit: 2 us
 constexpr int kExtra = 4;                                // an item's beginning and end: 8 us
+constexpr int kJoin = 16;                                // what cutting costs: a second beginning and the merge (2048 tokens over 32k: 962 us cut, 933 not)
 
 template <int D>
 struct Kernel {
@@ -44,17 +45,20 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   // where this workgroup's range begins
   int64_t total = 0, at = 0, end = 0;
   int N = 0, me = 0;
+  const auto take = [&](int n) {
+    N = n;
+    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
+    return me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+  };
   const auto begin = [&](int64_t all) {
     total = all;
-    N = (int)min((int64_t)kWorkgroups, total);             // workgroups with work: one unit at least
-    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
-    me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+    take((int)min((int64_t)kWorkgroups, total));           // workgroups with work: one unit at least
     at = me < N ? range_begin(total, N, me) : total;
     end = me < N ? range_begin(total, N, me + 1) : total;
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kKeys, kExtra>(p, begin, c)) {
+  if (!cursor_of_few<R, kKeys, kExtra, kJoin>(p, begin, take, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kKeys, kExtra>(p, cum);
     begin(cum[p.B]);
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   c.item = uniform(c.item);
-  int skip = uniform((int)c.skip), left = uniform((int)(end - at));      // shares of the item in front of the range; shares to do
+  int skip = uniform((int)c.skip), left = uniform(c.whole > 0 ? c.whole : (int)(end - at));      // shares of the item in front of the range; shares to do
 
   const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
   const bool second = wave >= kWaves / 2;

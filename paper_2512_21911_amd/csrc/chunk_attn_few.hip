@@ -75,6 +75,7 @@ struct FewBf16 {
   static constexpr int kOwn = 2 * kTileBytes;
   static constexpr int kLanesRows = 64 / kChunks, kPasses = kFewKeys / kLanesRows;      // rows that a wavefront loads at once
   static constexpr int kQueries = 16;                    // (bytes of LDS for the queries: none)
+  static constexpr int kJoin = 8;                        // what cutting costs (32 tokens, 8 KV heads over 1000 .. 1250: 39.8 us cut, 35.4 not)
   static constexpr int kExtra = 4;                       // an item's beginning and end, 3 us, in units of 0.8 us
   // (where a chunk of a row sits: as in the kernel for many rows)
   static __device__ __forceinline__ uint32_t k_at(int t, int c) {
@@ -164,6 +165,7 @@ struct FewF32 {
   static constexpr int kOwn = kFewKeys * kRowBytes;
   static constexpr int kLanesRows = 64 / kChunks, kPasses = kFewKeys / kLanesRows;
   static constexpr int kQueries = kFewRows * kRowBytes;
+  static constexpr int kJoin = 16;                       // (8 x 128 tokens, 8 heads over 600: 128 us cut, 102 not; d = 64 34.6, 27.3)
   static constexpr int kExtra = 8;                       // ... in units of 0.45 us (d = 64) and 0.9 us
   floatx4 k[D / 8], v[kPasses];
   Places<1> at;                                          // (of key lane mod 32)
@@ -263,17 +265,20 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
   // where this workgroup's range begins
   int64_t total = 0, at = 0, end = 0;
   int N = 0, me = 0;
+  const auto take = [&](int n) {
+    N = n;
+    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
+    return me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+  };
   const auto begin = [&](int64_t all) {
     total = all;
-    N = (int)min((int64_t)kWorkgroups, total);             // workgroups with work: one unit at least
-    // Consecutive ranges, which read the same keys, go to one XCD and its L2: workgroups are dealt to the eight in turn
-    me = N == kWorkgroups ? (int)(blockIdx.x % kXcds * (kWorkgroups / kXcds) + blockIdx.x / kXcds) : (int)blockIdx.x;
+    take((int)min((int64_t)kWorkgroups, total));           // workgroups with work: one unit at least
     at = me < N ? range_begin(total, N, me) : total;
     end = me < N ? range_begin(total, N, me + 1) : total;
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kFewKeys, kExtra>(p, begin, c)) {
+  if (!cursor_of_few<R, kFewKeys, kExtra, Unit::kJoin>(p, begin, take, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kFewKeys, kExtra>(p, cum);
     begin(cum[p.B]);
@@ -284,7 +289,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
   c.b = uniform(c.b);
   c.h = uniform(c.h);
   c.item = uniform(c.item);
-  int skip = uniform((int)c.skip), left = uniform((int)(end - at));
+  int skip = uniform((int)c.skip), left = uniform(c.whole > 0 ? c.whole : (int)(end - at));
 
   char* const mine = lds + wave * kOwn;
   while (skip + left > kExtra) {                             // (else the range ends in front of an item's units)

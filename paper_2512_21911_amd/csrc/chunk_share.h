@@ -99,6 +99,7 @@ struct Cursor {
   int b, h, item;            // where a range begins
   int64_t skip;              // shares of that item in front of it
   int64_t total;
+  int whole = 0;             // shares of the one item that the workgroup takes, where items aren't cut
 };
 // cum: [kMostB + 1] in LDS
 template <int R, int KEYS, int EXTRA>
@@ -192,9 +193,11 @@ __device__ __forceinline__ int shares_upto(const ChunkParams& p, const ChunkSeq&
 }
 
 // The same without LDS and barriers, by every wavefront for itself, for up to 64 sequences (lane b has sequence b) and groups of a power of two
-// of query heads, whose items' units have a sum in closed form.  `begin` says where the range begins, given the total.
-template <int R, int KEYS, int EXTRA, typename Begin>
-__device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
+// of query heads, whose items' units have a sum in closed form.  `begin` says where the range begins, given the total.  JOIN: shares that the end of an
+// item costs if it was cut; where no more workgroups than there are have an item each, and the largest is within that of an equal range, they aren't
+// cut (JOIN = 0: always); `take` says which, given how many there are.
+template <int R, int KEYS, int EXTRA, int JOIN, typename Begin, typename Take>
+__device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Take&& take, Cursor& c) {
   if (p.B > 64 || p.share_bound >= (1 << 30) || (p.G & (p.G - 1)) != 0 || p.G > R) return false;
   const int lane = threadIdx.x & 63;
   const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
@@ -206,6 +209,30 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Cursor& c) {
     if (lane >= d) upto += y;
   }
   c.total = __builtin_amdgcn_readlane(upto, 63);
+  if constexpr (JOIN > 0) {
+    int items_upto = n * p.Hkv, most = 0;
+    if (n > 0) most = Item<R, KEYS, EXTRA>(p, s, n - 1).shares;          // (an item in front of the last has more where the last has fewer rows)
+    if (n > 1) most = max(most, (int)Item<R, KEYS, EXTRA>(p, s, n - 2).shares);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int y = __shfl_up(items_upto, d, 64);
+      if (lane >= d) items_upto += y;
+      most = max(most, __shfl_xor(most, d, 64));
+    }
+    const int items = __builtin_amdgcn_readlane(items_upto, 63);
+    most = __builtin_amdgcn_readfirstlane(most);
+    if (items <= kWorkgroups && (int64_t)most * kWorkgroups <= c.total + JOIN * kWorkgroups) {
+      const int mine = take(items);
+      if (mine >= items) return true;
+      c.b = __builtin_ctzll(__ballot(items_upto > mine));
+      const int of_head = __builtin_amdgcn_readlane(n, c.b), rest = mine - (__builtin_amdgcn_readlane(items_upto, c.b) - of_head * p.Hkv);
+      c.h = (int)((uint32_t)rest / (uint32_t)of_head);
+      c.item = rest - c.h * of_head;
+      c.skip = 0;
+      c.whole = (int)Item<R, KEYS, EXTRA>(p, ChunkSeq{__builtin_amdgcn_readlane(s.len, c.b), 0, __builtin_amdgcn_readlane(s.n, c.b)}, c.item).shares;
+      return true;
+    }
+  }
   const int64_t at = begin(c.total);
   if (at >= c.total) return true;                          // (nothing for this workgroup)
   c.b = __builtin_ctzll(__ballot((int64_t)upto > at));

@@ -286,3 +286,13 @@ def test_offsets_past_32_bits():
     sh.n_pages = n_pages
     out, lse = call(sh, g)
     verify(sh, x, out, lse)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,Hkv,L,n", [(32, 8, 300, 1), (31, 8, 300, 1), (3, 2, 700, 130), (6, 2, 400, 200)])
+def test_items_of_like_size_are_not_cut(dtype, B, Hkv, L, n):
+    # no more items than workgroups, all about as large: each has a workgroup of its own; one far longer sequence among them, and they are cut
+    for longest in (L, 6000):
+        lens = [L + 3 * i for i in range(B)]
+        lens[B // 2] = longest
+        check(*build(lens, [max(1, n - 5 * i) for i in range(B)], dtype=dtype, Hq=4 * Hkv, Hkv=Hkv, d=64))
