@@ -1,16 +1,19 @@
 // Attention of new tokens over the cache (svf_chunk_attn), 32 query rows of a (sequence, KV head) at a time: bf16 with up to 32 of them, as for
 // single tokens, and everything in fp32.
+//   S = scale Q K^T, a running maximum m and sum l of each row:  O <- O 2^(m - m') + 2^(S - m') V,  l likewise,  out = O / l.
 //
-// The eight wavefronts of a workgroup have nothing to do with one another until the end of an item: each takes every eighth unit of 32 keys,
-// brings it into LDS of its own through registers, the next unit's chunks on their way while one is worked on (128 KB in flight on a
-// compute unit at d = 128), and keeps its own maximum, sum and output.  Then the eight are joined through LDS, and where an item was cut, the last
-// of its workgroups joins the parts.
-//   bf16  bound by memory, the cache goes by once.  The matrix cores still do both products (32 rows at a time, whatever of them is used), and
-//         have the time for weights of sixteen bits (two bf16 terms).
-//   fp32  bound by the fp32 matrix instructions (v_mfma_f32_32x32x2_f32: 64 cycles per 4096 operations, 157 TFLOP/s over the chip).  S^T = K Q^T
-//         leaves a query row in lane mod 32 with sixteen of the unit's keys per lane, which is the operand that O^T += V^T P^T takes, one
-//         register per step: the weights never leave their lanes.  K goes from memory into operand registers, the queries, the same for
-//         all wavefronts, wait in LDS.
+// The eight wavefronts of a workgroup have nothing to do with one another until the end of an item: each takes every eighth unit of 32 keys, the
+// next unit's loads on their way while one is worked on, and keeps its own maximum, sum and output.  Then the eight are joined through LDS, and where an
+// item was cut, the last of its workgroups joins the parts.
+//   bf16  bound by memory, the cache goes by once, 128 KB in flight on a compute unit at d = 128: 537 MB for four tokens over 32k in 109 us,
+//         4.9 TB/s (one token over 8k, 34 MB: 17 us, of which launch, first tiles and join are 10).  The matrix cores still do both products (32 rows
+//         at a time, whatever of them is used), and have the time for weights of sixteen bits (two bf16 terms): what is left of a weight behind
+//         its first term is rounded to bf16 too, 2^-17 of the weight.
+//   fp32  bound by the fp32 matrix instructions (v_mfma_f32_32x32x2_f32: 64 cycles per 4096 operations, 157 TFLOP/s over the chip; 32 keys in
+//         0.58 us at d = 64, 1.1 at d = 128, 0.43 and 0.85 at that rate).  S^T = K Q^T leaves a query row in lane mod 32 with sixteen of
+//         the unit's keys per lane, which is the operand that O^T += V^T P^T takes, one register per step: the weights never leave their lanes.
+//         K goes from memory into operand registers, V straight into LDS once the unit before has been read there (through registers there were
+//         too few of them: 1024 tokens, 8 heads, d = 128 109 us instead of 54), the queries, the same for all wavefronts, wait in LDS.
 #include "chunk_share.h"
 
 namespace svf {
@@ -105,6 +108,7 @@ struct FewBf16 {
       v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(V + off));
     }
   }
+  __device__ __forceinline__ void send(const char*, char*, int) {}
   // `next`: puts the next unit on its way, once this one's registers are free
   template <typename Next>
   __device__ __forceinline__ void work(char* own, const char*, int lane, float scale_log2, bool masked, int most, int least, float& m, float& l,
@@ -157,7 +161,7 @@ struct FewBf16 {
 };
 
 // fp32: a wavefront's part of LDS holds a unit's V, channel c of key t at c ^ 32 (t / 4 mod 2), since the halves of the wavefront read keys four
-// apart.  A lane's K is half of the 16-byte chunks of one key.
+// apart (a load to LDS writes lane after lane: the lanes' sources are exchanged instead).  A lane's K is half of the 16-byte chunks of one key.
 template <int D>
 struct FewF32 {
   typedef float Element;
@@ -165,10 +169,11 @@ struct FewF32 {
   static constexpr int kOwn = kFewKeys * kRowBytes;
   static constexpr int kLanesRows = 64 / kChunks, kPasses = kFewKeys / kLanesRows;
   static constexpr int kQueries = kFewRows * kRowBytes;
-  static constexpr int kJoin = 16;                       // (8 x 128 tokens, 8 heads over 600: 128 us cut, 102 not; d = 64 34.6, 27.3)
-  static constexpr int kExtra = 8;                       // ... in units of 0.45 us (d = 64) and 0.9 us
-  floatx4 k[D / 8], v[kPasses];
+  static constexpr int kJoin = 16;                       // (8 x 128 tokens, 8 heads over 600: 73 us cut, 49 not; d = 64 33, 24)
+  static constexpr int kExtra = 8;                       // ... in units of 0.6 us (d = 64) and 1.1 us
+  floatx4 k[D / 8];
   Places<1> at;                                          // (of key lane mod 32)
+  int64_t off;                                           // of that key's row of the unit that was requested last
 
   // chunk c of row r at c ^ (r mod 16): sixteen lanes read the same chunk of sixteen rows
   static __device__ __forceinline__ int q_at(int r, int c) { return r * kRowBytes + 16 * (c ^ (r & 15)); }
@@ -186,14 +191,19 @@ struct FewF32 {
     look_up_places(p, table, b, it, key0, lane & 31, 0, at);
   }
   __device__ __forceinline__ void request(const ChunkParams& p, const char* K, const char* V, int lane) {
-    const int64_t off = 4 * ((int64_t)at.slot[0] * p.kv.stride_tok + (int64_t)inside(p, at.page[0]) * p.kv.stride_page);
+    off = 4 * ((int64_t)at.slot[0] * p.kv.stride_tok + (int64_t)inside(p, at.page[0]) * p.kv.stride_page);
 #pragma unroll
     for (int c = 0; c < D / 8; ++c) k[c] = *reinterpret_cast<const floatx4*>(K + off + 16 * (2 * c + (lane >> 5)));
+  }
+  // the values of the unit that was requested, straight into LDS, where those of the unit before have been read
+  __device__ __forceinline__ void send(const char* V, char* own, int lane) {
+    const int t_lane = lane / kChunks, c = lane % kChunks;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const int64_t row = __shfl((long long)off, lane / kChunks + i * kLanesRows, 64);
-      v[i] = *reinterpret_cast<const floatx4*>(V + row + 16 * (lane % kChunks));
-      __builtin_amdgcn_sched_barrier(0);                  // (one address at a time)
+      const int t = t_lane + i * kLanesRows;
+      const int64_t row = __shfl((long long)off, t, 64);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(V + row + 16 * (c ^ (8 * ((t >> 2) & 1)))),
+                                       (__attribute__((address_space(3))) uint32_t*)(own + i * 1024), 16, 0, 0);
     }
   }
   template <typename Next>
@@ -219,11 +229,7 @@ struct FewF32 {
         for (int e = 0; e < 4; ++e) s[e & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[2 * g + c][e], q[g & 1][c][e], s[e & 1], 0, 0, 0);
       SVF_IN_ORDER();
     }
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      const int t = lane / kChunks + i * kLanesRows, c = 4 * (lane % kChunks);
-      *reinterpret_cast<floatx4*>(vs + t * D + (c ^ (32 * ((t >> 2) & 1)))) = v[i];
-    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): the unit's values are in LDS
     floatx16 x = s[0] + s[1];
     SVF_IN_ORDER();
     next();
@@ -307,6 +313,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
     if (wave < n) {
       look_up(wave);
       unit.request(p, K, V, lane);
+      unit.send(V, mine, lane);
       if (wave + kWaves < n) look_up(wave + kWaves);
     }
     // this lane's row
@@ -327,6 +334,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
                     if (u + 2 * kWaves < n) look_up(u + 2 * kWaves);
                   }
                 });
+      if (u + kWaves < n) unit.send(V, mine, lane);
     }
 
     // the wavefronts' results joined: each leaves its own in its part of LDS
