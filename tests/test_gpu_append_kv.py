@@ -215,3 +215,22 @@ def test_captured_and_replayed_on_another_stream():
         assert torch.equal(q_out, want[1])
         written = g["K"].abs().sum(-1) > 0
         assert torch.equal(g["K"][written], want[0][written]) and int(written.sum()) == 5 * sh.Hkv
+
+
+def test_more_rows_than_a_grid_has_threads_in_x():
+    # (workgroups of 256 threads, one to four rows each; one sequence, in the last rows)
+    n_rows, n = (1 << 26) + 7, 6
+    sh, x = build([3], [n], Hq=1, Hkv=1, d=64, rotary=64, packed=False)
+    K, V = x["K"].cuda(), x["V"].cuda()
+    big = [torch.empty(n_rows, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for b, name in zip(big, "kv"):
+        b[-n:] = x[name].cuda()
+    sh.n_rows = n_rows
+    S.svf_append_kv(sh, big[0], big[1], x["table"].cuda(), x["seq_lens"].cuda(), torch.tensor([n_rows - n], dtype=torch.int32, device="cuda"),
+                    x["new_lens"].cuda(), K, V, inv_freq=x["inv_freq"].cuda())
+    small = dict(K=x["K"].cuda(), V=x["V"].cuda())
+    sh.n_rows = n
+    S.svf_append_kv(sh, x["k"].cuda(), x["v"].cuda(), x["table"].cuda(), x["seq_lens"].cuda(), x["new_rows"].cuda(), x["new_lens"].cuda(),
+                    small["K"], small["V"], inv_freq=x["inv_freq"].cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(K, small["K"]) and torch.equal(V, small["V"]) and not torch.equal(K, x["K"].cuda())
