@@ -93,8 +93,9 @@ size_t svf_chunk_workspace_bytes(const svf_chunk_shape_t* shape);
  * h / (Hq / Hkv) under one softmax with scale sm_scale.  lse_or_null is optional.  `out` must
  * not overlap q or the cache.
  * Arithmetic in bf16: products accumulate in fp32, softmax weights are rounded to bf16 before they
- * multiply V, their sum is taken in fp32 from the unrounded ones, everything else stays fp32 until the output
- * is rounded once.  fp32 shapes are fp32 throughout.  The same bits from call to call.
+ * multiply V (where max_new * Hq / Hkv <= 32 to sixteen bits), their sum is taken in fp32 from the unrounded ones, everything
+ * else stays fp32 until the output is rounded once.  fp32 shapes are fp32 throughout.  The same bits from call to call.
+ * That limit also chooses the kernel: a step of single tokens is served 1.5 times as fast by a shape whose max_new says so.
  */
 int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K, const void* V,
                    const int32_t* block_table, const int32_t* seq_lens, const int32_t* new_rows,

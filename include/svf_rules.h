@@ -80,7 +80,7 @@ size_t svf_sample_workspace_bytes(int32_t rows, int32_t V);
  *   probs        fp32  [rows][V], the kept weights over their total, zero elsewhere: what svf_accept_resample takes
  * u and tokens are given both or not at all, and tokens or probs at least.  Logits of -inf (masked tokens) have
  * weight zero, NaN counts as -inf; a row of nothing else gets token -1 and probabilities of zero.
- * A weight is good to 2^-27 of itself; sums are of whole numbers or in 64 bits in a fixed order: the same bits from call to call.
+ * A weight is good to 2^-27 of itself (where it is below e^-16 of the largest: 2^-18); sums are of whole numbers or in 64 bits in a fixed order: the same bits from call to call.
  * A temperature below 2^-60 counts as that; logits above 2^122 (temperatures below one: 2^122 temperatures) weigh the same.
  */
 int svf_sample(const void* logits, int32_t dtype, int64_t logits_stride, int32_t rows, int32_t V,

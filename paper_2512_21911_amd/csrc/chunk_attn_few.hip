@@ -8,7 +8,7 @@
 //   bf16  bound by memory, the cache goes by once, 128 KB in flight on a compute unit at d = 128: 537 MB for four tokens over 32k in 109 us,
 //         4.9 TB/s (one token over 8k, 34 MB: 17 us, of which launch, first tiles and join are 10).  The matrix cores still do both products (32 rows
 //         at a time, whatever of them is used), and have the time for weights of sixteen bits (two bf16 terms): what is left of a weight behind
-//         its first term is rounded to bf16 too, 2^-17 of the weight.
+//         its first term is rounded to bf16 too, 2^-16 of the weight.
 //   fp32  bound by the fp32 matrix instructions (v_mfma_f32_32x32x2_f32: 64 cycles per 4096 operations, 157 TFLOP/s over the chip; 32 keys in
 //         0.58 us at d = 64, 1.1 at d = 128, 0.43 and 0.85 at that rate).  S^T = K Q^T leaves a query row in lane mod 32 with sixteen of
 //         the unit's keys per lane, which is the operand that O^T += V^T P^T takes, one register per step: the weights never leave their lanes.

@@ -1,25 +1,27 @@
 // Sampling from logits (svf_sample): temperature, top-k, top-p, min-p, and the draw by inversion.
 //
 // All three filters keep a prefix of the tokens in descending order of their logits (ties by index), so what a row keeps
-// is two numbers, a border: the key of the last kept logit and the index of the last kept token with it.  Nothing is sorted
-// but the few tokens around it.  A row is cut into slices, and three launches find border and token:
-//   stats    a workgroup per slice reads its logits once, into registers: their maximum and the sum of their weights or, if the row has a
-//            filter, a histogram of counts and weights over 1023 bins of logits from the maximum down.
-//   gather   every workgroup adds up the row's histograms for itself and knows the bin the border is in; it reads its slice again only if
-//            it has tokens there, and writes those to the row's list (top-k: all from the top on, so that
-//            the mass that top-p takes its share of is at hand).
-//   draw     a workgroup per row sorts the list, walks it to the border, adds up what every slice keeps, and walks the one slice the
-//            target falls in.
-// and a fourth, with a workgroup per slice again, writes the probabilities where they are asked for.
-// A row whose border bin has more tokens than the list (many equal logits, a top-k of thousands) is settled in the third launch by
+// is two numbers, a border: the last kept logit and the index of the last kept token with it.  Nothing is sorted but the few tokens around it.
+// A row is cut into slices of up to 32 768 logits, which a workgroup holds in registers, and three steps find border and token:
+//   stats    of a slice: the maximum and the sum of the weights or, if the row has a filter, a histogram of counts and weights over 1023 bins of
+//            logits from the maximum down.
+//   gather   the row's histograms are added up, and the bin is known that the border is in; the tokens in it go to the row's list (top-k: all from
+//            the top on, so that the mass that top-p takes its share of is at hand).
+//   draw     the list is sorted and walked to the border, what every slice keeps is added up, and the token is found: by the
+//            list alone if everything kept is in it, else in the one slice that the target falls in.
+// A row of one slice has all three in one launch (32 000 logits, top-k and top-p: 16 us; in three launches over eight slices 19), longer rows in
+// three: a workgroup per slice, per slice (which reads its slice again if it has tokens for the list), per row.  A fourth, with a workgroup per
+// slice again, writes the probabilities where they are asked for.
+// A row whose border bin has more tokens than the list (many equal logits, a top-k of thousands) is settled in the third step by
 // radix selection over the whole row.
 //
 // Weights.  Bins are a power of two of logits wide, at whole multiples of it, so a logit's bin and its place in the bin are exact in fp32.  A
 // weight is its bin's, 2^(-bin c) in fp64, times 2^(place c), place c < 0.046: a short polynomial in fp32 whose rounding is 2^-24 of the
 // excess over one.  That is good to 2^-27, which an fp32 exponential of the whole argument is not (2^-20 at 20 below the maximum), and a hundred
-// thousand tokens' borders wait for the target in between; and a histogram adds whole numbers, count and weight in one 64-bit word.
-// (With fp64 arithmetic per logit and separate words the first launch took 20.1 instead of 16.9 us for 64 rows of 129 280 fp32 logits.)
-// Bound: the logits, once from memory and, where the border's bin is gathered and the slice walked, again from the caches.
+// thousand tokens' borders wait for the target in between; and a histogram adds whole numbers, count and weight in one 64-bit word, so that
+// the order of the adding does not matter.
+// Bound: for few rows by the steps' chains of barriers and reads (10 us for 4000 logits); for many by the vector instructions of the first step
+// (256 rows of 129 280 in bf16: 31 us, 66 MB), the second's (29 us), and one workgroup a row in the third (20 us); the probabilities, 198 MB, take 40 us.
 #include <hip/hip_bf16.h>
 #include <hip/hip_runtime.h>
 
@@ -113,7 +115,7 @@ __device__ __forceinline__ float4 logits4(const T* x, int v, int end) {
   return f;
 }
 // Tokens v0 + 4 (i THREADS + thread) .. + 3 of all i < N.  Whether all threads' are inside the row is the same for the workgroup, and then the
-// loads are under no mask: under one they wait for each other (16.9 us instead of 13.x for the first launch at 64 rows of 129 280).
+// loads are under no mask: under one they wait for each other (16.9 us instead of 16.1 for the first launch at 64 rows of 129 280).
 template <int N, int THREADS, typename T>
 __device__ __forceinline__ void read_logits(const T* x, int v0, int thread, int end, float4 (&f)[N]) {
 #pragma unroll
