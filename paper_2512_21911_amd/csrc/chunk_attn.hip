@@ -88,8 +88,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
   const int c_lane = tid % C::kChunks, t_lane = tid / C::kChunks;
   const bool second = wave >= kWaves / 2;
   while (skip + left > kExtra) {                             // (else the range ends in front of an item's units)
-    ChunkSeq s = load_seq(p, c.b);
-    s = {uniform(s.len), uniform(s.row), uniform(s.n)};
+    const ChunkSeq s{uniform(c.seq.len), uniform(c.seq.row), uniform(c.seq.n)};
     const Item<R, kKeys, kExtra> it(p, s, c.item);
     const Part part(it, skip, left);
     const int n = part.end - part.begin, unit0 = it.unit0 + part.begin;
@@ -383,8 +382,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       c.item = 0;
       if (++c.h == p.Hkv) {
         c.h = 0;
-        ++c.b;
-        while (left > 0 && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with shares: some are left)
+        if (left > 0) {
+          do c.seq = load_seq(p, ++c.b); while (c.seq.n == 0);             // (there is one with shares: some are left)
+        }
       }
     }
   }

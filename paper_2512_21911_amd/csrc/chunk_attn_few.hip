@@ -299,8 +299,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
 
   char* const mine = lds + wave * kOwn;
   while (skip + left > kExtra) {                             // (else the range ends in front of an item's units)
-    ChunkSeq s = load_seq(p, c.b);
-    s = {uniform(s.len), uniform(s.row), uniform(s.n)};
+    const ChunkSeq s{uniform(c.seq.len), uniform(c.seq.row), uniform(c.seq.n)};
     const Item<R, kFewKeys, kExtra> it(p, s, c.item);
     const Part part(it, skip, left);
     const int n = part.end - part.begin, unit0 = it.unit0 + part.begin;
@@ -464,8 +463,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_few_kernel(ChunkParams
       c.item = 0;
       if (++c.h == p.Hkv) {
         c.h = 0;
-        ++c.b;
-        while (left > 0 && load_seq(p, c.b).n == 0) ++c.b;               // (there is one with shares: some are left)
+        if (left > 0) {
+          do c.seq = load_seq(p, ++c.b); while (c.seq.n == 0);             // (there is one with shares: some are left)
+        }
       }
     }
   }

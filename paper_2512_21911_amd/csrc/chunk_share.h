@@ -99,6 +99,7 @@ struct Cursor {
   int b, h, item;            // where a range begins
   int64_t skip;              // shares of that item in front of it
   int64_t total;
+  ChunkSeq seq;              // sequence b
   int whole = 0;             // shares of the one item that the workgroup takes, where items aren't cut
 };
 // cum: [kMostB + 1] in LDS
@@ -158,7 +159,20 @@ __device__ Cursor cursor_at(const ChunkParams& p, const int64_t* cum, int64_t at
     rest -= lane64(x, 63);
   }
   c.skip = rest;
+  c.seq = s;
   return c;
+}
+
+// Scans over a wavefront's lanes by moves inside a row of sixteen and from row to row: no trips through LDS.
+template <typename Join>
+__device__ __forceinline__ int wave_scan(int x, Join&& join) {
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));     // row_shr:1, 2, 4, 8
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));    // row_bcast:15 -> rows 1, 3
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));    // row_bcast:31 -> rows 2, 3
+  return x;
 }
 
 constexpr int kWorkgroups = 256;                         // one on each compute unit
@@ -202,25 +216,18 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Take&& take, 
   const int lane = threadIdx.x & 63;
   const ChunkSeq s = load_seq(p, min(lane, p.B - 1));
   const int n = lane < p.B ? items_of<R>(p, s) : 0, of_seq = n > 0 ? shares_upto<R, KEYS, EXTRA>(p, s, n) : 0;
-  int upto = of_seq * p.Hkv;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += y;
-  }
+  const auto add = [](int x, int y) { return x + y; };
+  const auto seq_at = [&](int b) {
+    return ChunkSeq{__builtin_amdgcn_readlane(s.len, b), __builtin_amdgcn_readlane(s.row, b), __builtin_amdgcn_readlane(s.n, b)};
+  };
+  const int upto = wave_scan(of_seq * p.Hkv, add);
   c.total = __builtin_amdgcn_readlane(upto, 63);
   if constexpr (JOIN > 0) {
-    int items_upto = n * p.Hkv, most = 0;
+    int most = 0;
     if (n > 0) most = Item<R, KEYS, EXTRA>(p, s, n - 1).shares;          // (an item in front of the last has more where the last has fewer rows)
     if (n > 1) most = max(most, (int)Item<R, KEYS, EXTRA>(p, s, n - 2).shares);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(items_upto, d, 64);
-      if (lane >= d) items_upto += y;
-      most = max(most, __shfl_xor(most, d, 64));
-    }
-    const int items = __builtin_amdgcn_readlane(items_upto, 63);
-    most = __builtin_amdgcn_readfirstlane(most);
+    const int items_upto = wave_scan(n * p.Hkv, add), items = __builtin_amdgcn_readlane(items_upto, 63);
+    most = __builtin_amdgcn_readlane(wave_scan(most, [](int x, int y) { return max(x, y); }), 63);       // (none is negative)
     if (items <= kWorkgroups && (int64_t)most * kWorkgroups <= c.total + JOIN * kWorkgroups) {
       const int mine = take(items);
       if (mine >= items) return true;
@@ -229,7 +236,8 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Take&& take, 
       c.h = (int)((uint32_t)rest / (uint32_t)of_head);
       c.item = rest - c.h * of_head;
       c.skip = 0;
-      c.whole = (int)Item<R, KEYS, EXTRA>(p, ChunkSeq{__builtin_amdgcn_readlane(s.len, c.b), 0, __builtin_amdgcn_readlane(s.n, c.b)}, c.item).shares;
+      c.seq = seq_at(c.b);
+      c.whole = (int)Item<R, KEYS, EXTRA>(p, c.seq, c.item).shares;
       return true;
     }
   }
@@ -240,7 +248,7 @@ __device__ bool cursor_of_few(const ChunkParams& p, Begin&& begin, Take&& take, 
   int rest = (int)at - (__builtin_amdgcn_readlane(upto, c.b) - per_head * p.Hkv);
   c.h = (int)((uint32_t)rest / (uint32_t)per_head);
   rest -= c.h * per_head;
-  const ChunkSeq t{__builtin_amdgcn_readlane(s.len, c.b), 0, __builtin_amdgcn_readlane(s.n, c.b)};
+  const ChunkSeq t = c.seq = seq_at(c.b);
   int lo = 0, hi = __builtin_amdgcn_readlane(n, c.b) - 1;  // the last item with no more than `rest` shares in front of it
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
