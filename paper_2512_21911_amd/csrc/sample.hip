@@ -26,6 +26,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "svf_device.h"
@@ -310,6 +311,7 @@ __device__ __forceinline__ float block_max(float x, float* sh) {
   __syncthreads();
   return x;
 }
+
 // ---- stats -----------------------------------------------------------------------------------------
 
 constexpr uint64_t kExcessMask = (1ull << kCountAt) - 1;
@@ -868,8 +870,15 @@ __device__ __forceinline__ void draw_row(const SampleParams& p, int r, const T* 
   if (lane == 0) sh.scan[wave] = sum;
   __syncthreads();
   const uint64_t upto_wave = wave_scan64(lane < kWaves ? sh.scan[lane] : 0), in_all = lane64(upto_wave, kWaves - 1);
-  if (in_all == 0) {
-    if (tid == 0) p.tokens[r] = border.index >= 0 && border.index < p.V ? border.index : begin;
+  if (in_all == 0) {                                     // (a slice whose weights are something together, and nothing each: its first kept token)
+    if (tid == 0) sh.index = INT_MAX;
+    __syncthreads();
+    for (int v = begin + tid; v < end; v += kThreads) {
+      float l = load1(x + v);
+      if (border.keeps(l, v)) atomicMin(&sh.index, v);
+    }
+    __syncthreads();
+    if (tid == 0) p.tokens[r] = sh.index < p.V ? sh.index : begin;
     return;
   }
   // (the bins' weights, rounded once each, may add up to a little more than the tokens': then it is the slice's last)

@@ -136,6 +136,15 @@ def test_rows_of_the_lowest_value_and_nothing(dtype, V):
           top_k=torch.tensor([0, 7, 0, 0, 0, 7], dtype=torch.int32), top_p=torch.tensor([1.0, 1.0, 0.5, 0.9, 1.0, 0.4]))
 
 
+def test_the_lowest_target_is_no_masked_token():
+    # a stretch of tokens 35 below the others, the first of it masked: their weights are something together, and nothing each
+    lg = torch.zeros(3, 40000)
+    lg[:, :5000] = -35.0
+    lg[0, 0] = lg[1, :7] = -float("inf")
+    check(lg, torch.zeros(3))
+    check(lg[:, :9000].contiguous(), torch.zeros(3), top_p=torch.tensor([0.9, 1.0, 0.9]))
+
+
 def test_extreme_settings():
     lg, u = rows(8, 2000, seed=4)
     check(lg, u, temperature=[1e-30, 1e-4, 1e4, 3e38, float("inf"), 1.0, 1.0, 1.0], top_k=[0, 0, 0, 0, 0, -3, 1999, 2 ** 31 - 1])
