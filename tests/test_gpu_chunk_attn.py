@@ -296,3 +296,14 @@ def test_items_of_like_size_are_not_cut(dtype, B, Hkv, L, n):
         lens = [L + 3 * i for i in range(B)]
         lens[B // 2] = longest
         check(*build(lens, [max(1, n - 5 * i) for i in range(B)], dtype=dtype, Hq=4 * Hkv, Hkv=Hkv, d=64))
+
+
+def test_shapes_of_both_kernels_share_a_workspace():
+    cases = [build([300, 20], [200, 130], Hq=8, Hkv=2, d=128, seed=1), build([3000, 5], [1, 1], Hq=8, Hkv=2, d=128, seed=2),
+             build([900], [40], Hq=4, Hkv=1, d=64, dtype=torch.float32, seed=3), build([2000, 70, 0], [1, 3, 2], Hq=8, Hkv=2, d=64, seed=4)]
+    alone = [call(sh, to_gpu(x)) for sh, x in cases]
+    ws = max((S.new_chunk_workspace(sh) for sh, _ in cases), key=lambda w: w.numel())
+    for i in (0, 1, 2, 3, 1, 0, 3, 2, 0, 1):
+        sh, x = cases[i]
+        out, lse = call(sh, to_gpu(x), ws=ws)
+        assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1])
