@@ -250,7 +250,6 @@ def prepare(c, seed):
             v_stride=stride, rotary_dim=c.get("rotary", 0), rotary_interleaved=c.get("interleaved", False))
         if c["kind"] == "append":
             s["q_out"] = torch.empty_strided(s["q"].shape, s["q"].stride(), dtype=dt, device="cuda") if c["rotary"] else None
-            s["written"] = _tokens(s)[2] if c["rotary"] and c["slots"] else None                     # (the others are gaps)
         else:
             s["ws"] = S.new_chunk_workspace(s["shape"])
             s["out"] = torch.empty_like(s["q"])
@@ -358,7 +357,7 @@ def run(s):
     if kind == "append":
         S.svf_append_kv(s["shape"], s["k"], s["v"], s["table"], s["seq_lens"], s["new_rows"], s["new_lens"], s["K"], s["V"],
                         q=s["q"], q_out=s["q_out"], inv_freq=s["inv_freq"])
-        return {"K": s["K"], "V": s["V"], "q": s["q_out"] if s["written"] is None else s["q_out"][s["written"]]}
+        return {"K": s["K"], "V": s["V"], "q": s["q_out"]}
     if kind == "chunk":
         S.svf_chunk_attn(s["shape"], s["q"], s["K"], s["V"], s["table"], s["seq_lens"], s["new_rows"], s["new_lens"], s["out"],
                          s["ws"], lse=s["lse"])
