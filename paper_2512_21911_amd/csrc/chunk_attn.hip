@@ -259,12 +259,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, sc[0][i]), sc[1][i]);
       top = halves_max(top);
-      float up = 0.f;                                      // (a row whose keys so far are all masked keeps -inf and weights of zero)
+      float up = 0.f, f = 1.f;                             // (a row whose keys so far are all masked keeps -inf and weights of zero)
       if (top > -INFINITY) {
-        up = m == -INFINITY ? top : fmaxf(top, 0.f);
-        m = (m == -INFINITY ? 0.f : m) + up;
+        if (m == -INFINITY) {                              // l and o are zero, and 2^-up may be infinite
+          up = m = top;
+        } else {
+          up = fmaxf(top, 0.f);
+          m += up;
+          f = __builtin_amdgcn_exp2f(-up);
+        }
       }
-      const float f = __builtin_amdgcn_exp2f(-up);
       l *= f;
 #pragma unroll
       for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;

@@ -307,3 +307,16 @@ def test_shapes_of_both_kernels_share_a_workspace():
         sh, x = cases[i]
         out, lse = call(sh, to_gpu(x), ws=ws)
         assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,news,window", [([0], [64], 0), ([0, 70], [200, 65], 1), ([3, 300], [130, 90], 50), ([0, 1500], [260, 300], 0),
+                                              ([0, 63, 5], [1, 2, 1], 0)])
+@pytest.mark.parametrize("level", [7.0, 30.0])
+def test_scores_far_below_zero(dtype, d, lens, news, window, level):
+    """The first keys that a row sees score -100 and less: what it has summed until then, nothing, stays nothing."""
+    sh, x = build(lens, news, dtype=dtype, d=d, window=window)
+    x["K"] = (x["K"] * 0.125 + 2.0).to(dtype)
+    x["q"] = (x["q"].abs() * 0.25 - level).to(dtype)       # scores of -2 (level - 0.2) sqrt(d)
+    check(sh, x)
