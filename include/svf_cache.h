@@ -11,7 +11,8 @@
  * owned by the caller; work is enqueued on `stream` and the call returns immediately; 0 on
  * success, a negative SVF_ERR_* code (svf.h) otherwise, checked before any launch; inputs must be
  * finite (a NaN or infinity in a query stays in that query's output, one in a cached token spoils
- * the new tokens of sequences that see it; cache places that no new token sees may hold anything).
+ * the new tokens of sequences that see it; cache places that no new token sees may hold anything), and
+ * values below 2^125 / (tokens of the sequence + 64), since their weighted sums are fp32 until they are divided.
  * A call runs on the current device, as every HIP launch does: stream and pointers are that device's.
  *
  * Tensors (last index fastest; element type = shape.dtype unless said otherwise):

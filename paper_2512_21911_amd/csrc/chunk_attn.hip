@@ -226,9 +226,10 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       __builtin_amdgcn_sched_barrier(0);
     };
     // A unit's scores into weights, 2^(score - m), and their sum into l.  m need not be the maximum: weights, sums and outputs are
-    // floating point, and good as long as nothing overflows.  So the maximum of the first unit that a row sees serves until a unit's weights
-    // sum to more than 2^40 in some row (the sums are there anyway; looking for the maximum of every unit cost a tenth of the time),
-    // and then the unit is done again with the maximum it has.
+    // floating point, and good as long as nothing overflows.  So the maximum of the first unit that a row sees serves until a lane's weights of
+    // a unit sum to more than 2^8 (the sums are there anyway; looking for the maximum of every unit cost a tenth of the time),
+    // and then the unit is done again with the maximum it has.  A key weighs no more than 8 on average: values have nearly the range that weights of at
+    // most one leave them.
     const auto exponents = [&](float use) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
         unseen = __ballot(m == -INFINITY) != 0;
       }
       float sum = exponentials();
-      if (__ballot(sum > 0x1p40f)) {
+      if (__ballot(sum > 0x1p8f)) {
         rebase();
         sum = exponentials();
       }

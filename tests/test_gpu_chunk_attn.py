@@ -320,3 +320,16 @@ def test_scores_far_below_zero(dtype, d, lens, news, window, level):
     x["K"] = (x["K"] * 0.125 + 2.0).to(dtype)
     x["q"] = (x["q"].abs() * 0.25 - level).to(dtype)       # scores of -2 (level - 0.2) sqrt(d)
     check(sh, x)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rise", [0.1, 0.3, 1.0])
+def test_large_values_under_rising_scores(dtype, d, rise):
+    """Values of up to 2^125 / (tokens + 64), scores that rise by 0.1 to 1 a key: weights relative to an early key stay small enough."""
+    sh, x = build([900] * 6, [40] * 6, dtype=dtype, Hq=8, Hkv=8, d=d, page=0)   # (items that are not cut)
+    slots = x["K"].shape[1]
+    x["K"] = (x["K"] * 0.01 + rise * d ** -0.5 * torch.arange(slots)[None, :, None, None]).to(dtype)
+    x["q"] = torch.ones_like(x["q"])
+    x["V"] = (x["V"].clamp(-4, 4) * 2.0 ** 112).to(dtype)  # 4 x 2^112 x (940 + 64) < 2^125
+    check(sh, x)
