@@ -490,7 +490,8 @@ struct ListRange {
   __device__ __forceinline__ ListRange(const Settings& set, float top, Bins list) {
     const double first = (double)set.bin_of(top), lower = first - list.hi, past = first - list.lo + 1;
     least = lower <= -(double)kFar ? -3.402823466e38f : at_least(lower / (double)set.per_bin);
-    most = past >= (double)kFar ? INFINITY : nextafterf(at_least(past / (double)set.per_bin), -INFINITY);
+    // (no logit is above the first bin; its end has no number where bins are counted past 2^53, and a list further down begins far below that)
+    most = list.lo == 0 ? INFINITY : nextafterf(at_least(past / (double)set.per_bin), -INFINITY);
   }
   __device__ __forceinline__ bool has(float l) const { return l >= least && l <= most; }           // (never NaN)
 };

@@ -237,3 +237,19 @@ def test_distributions_feed_acceptance():
     for b in range(B):
         if int(n[b]) < gamma:
             assert float(pt[b * gamma + int(n[b]), int(again[b])]) > 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [900, 9000, 40000])
+@pytest.mark.parametrize("scale,temperature", [(1.0, 1e-13), (1.0, 1e-14), (1.0, 1e-20), (1.0, 1e-30), (1e14, 1.0), (1e15, 1.0), (1e15, 1e-3),
+                                               (1e15, 1e15), (1e30, 1.0), (1e30, 0.0), (-1e15, 1.0)])
+def test_filters_where_bins_are_counted_past_53_bits(dtype, V, scale, temperature):
+    """Filters at temperatures near none and with logits of any size: a row's maximum is among what it keeps."""
+    lg, u = rows(8, V, seed=V, dtype=dtype)
+    lg = (lg.float() * abs(scale)).to(dtype)
+    if scale < 0:                                          # all far below zero
+        lg = -lg.abs()
+    lg[1, 7::11] = lg[1].max()                             # (ties at the top)
+    check(lg, u, temperature=[temperature] * 8, top_k=[1, 1, 5, 0, 0, 0, 40, 0], top_p=[1.0, 1.0, 1.0, 0.9, 1.0, 0.5, 0.3, 1.0],
+          min_p=[0.0, 0.0, 0.0, 0.0, 0.1, 0.9, 0.01, 1.0])
+    check(lg, u, temperature=[0.0] * 8, probs=False)
