@@ -9,7 +9,8 @@
 // arguments included, and does no arithmetic.  A tensor argument may be None (NULL) and is otherwise a
 // tensor or any object with its data_ptr() (and numel() or shape where a call needs them); a shape is an
 // instance of the ctypes structure that mirrors the C one, and of no other (a buffer of the right size would do
-// for the pointer, with its fields read as something else); work is enqueued on torch's current stream.
+// for the pointer, with its fields read as something else); svf_sample, which has its sizes from one tensor, looks at the others'
+// element types and sizes; work is enqueued on torch's current stream.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <c10/hip/HIPStream.h>
@@ -221,6 +222,21 @@ Rows rows_of(const Signature& s, const Args& a, int i) {
   return {dtype, (int32_t)t.size(0), (int32_t)t.size(1), t.size(0) > 1 ? t.stride(0) : 0};
 }
 
+// Where the sizes come from another argument: a tensor (or None) of this element type, contiguous, with `least` elements or more.
+void holds(const Signature& s, const Args& a, int i, at::ScalarType type, int64_t least) {
+  if (!a.obj[i] || !THPVariable_Check(a.obj[i])) return;
+  const at::Tensor& t = THPVariable_Unpack(a.obj[i]);
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s(): %s must be %s, not %s", s.where, s.params[i].name, c10::toString(type),
+                 c10::toString(t.scalar_type()));
+    throw Failed{};
+  }
+  if (t.numel() < least || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s(): %s must be contiguous, with %lld elements", s.where, s.params[i].name, (long long)least);
+    throw Failed{};
+  }
+}
+
 template <typename Shape>
 const Shape* shape_of(const Args& a, int i) { return static_cast<const Shape*>(a.ptr[i]); }
 
@@ -346,7 +362,11 @@ SVF_CALL(svf_chunk_attn,
          tensor("new_rows"), tensor("new_lens"), tensor("out"), workspace("ws"), tensor_or_none("lse"))
 
 SVF_CALL(svf_sample,
-         const Rows d = rows_of(s, a, 0); void* st = stream(); NoGil free;
+         const Rows d = rows_of(s, a, 0);
+         for (int i : {1, 4, 6, 7}) holds(s, a, i, at::kFloat, d.rows);
+         for (int i : {2, 5}) holds(s, a, i, at::kInt, d.rows);
+         holds(s, a, 8, at::kFloat, (int64_t)d.rows * d.columns);
+         void* st = stream(); NoGil free;
          rc = svf_sample(a.ptr[0], d.dtype, d.stride, d.rows, d.columns, F32(4), I32(5), F32(6), F32(7), F32(1),
                          static_cast<int32_t*>(a.ptr[2]), static_cast<float*>(a.ptr[8]), WS(3), st),
          tensor("logits"), tensor("u"), tensor("tokens"), workspace("ws"), tensor_or_none("temperature"),

@@ -128,3 +128,30 @@ def test_python_arguments():
                                       kv_strides=(64, 64, 64)), *[None] * 9)
     with pytest.raises(TypeError):
         S.svf_append_kv(good(), None)
+
+
+def test_sampling_arguments_have_the_types_and_sizes_that_are_read():
+    """(CPU tensors: every call is refused by the binding.)"""
+    import torch
+    R, V = 4, 9
+    good = dict(logits=torch.zeros(R, V), u=torch.zeros(R), tokens=torch.zeros(R, dtype=torch.int32), temperature=torch.ones(R),
+                top_k=torch.ones(R, dtype=torch.int32), top_p=torch.ones(R), min_p=torch.ones(R), probs=torch.zeros(R, V))
+
+    def call(**kw):
+        S.svf_sample(**{**good, **kw}, ws=torch.empty(0, dtype=torch.uint8))
+    for n in ("u", "temperature", "top_p", "min_p", "probs"):
+        for dt in (torch.float64, torch.bfloat16, torch.int32):
+            with pytest.raises(TypeError, match=n):
+                call(**{n: good[n].to(dt)})
+    for n in ("tokens", "top_k"):
+        for dt in (torch.int64, torch.float32, torch.int16):
+            with pytest.raises(TypeError, match=n):
+                call(**{n: good[n].to(dt)})
+    for n, x in good.items():
+        if n != "logits":
+            with pytest.raises(ValueError, match=n):
+                call(**{n: x[:R - 1]})
+            with pytest.raises(ValueError, match=n):
+                call(**{n: torch.stack((x, x), -1)[..., 0]})
+    with pytest.raises(ValueError, match="probs"):
+        call(probs=torch.zeros(R, V - 1))

@@ -253,3 +253,14 @@ def test_filters_where_bins_are_counted_past_53_bits(dtype, V, scale, temperatur
     check(lg, u, temperature=[temperature] * 8, top_k=[1, 1, 5, 0, 0, 0, 40, 0], top_p=[1.0, 1.0, 1.0, 0.9, 1.0, 0.5, 0.3, 1.0],
           min_p=[0.0, 0.0, 0.0, 0.0, 0.1, 0.9, 0.01, 1.0])
     check(lg, u, temperature=[0.0] * 8, probs=False)
+
+
+def test_buffers_longer_than_the_batch():
+    lg, u = rows(3, 5000, seed=41)
+    want = run(lg, u, top_k=[40] * 3)
+    tokens, probs = torch.full((8,), -9, dtype=torch.int32, device="cuda"), torch.full((8, 5000), 5.0, device="cuda")
+    S.svf_sample(lg.cuda(), torch.cat((torch.as_tensor(u), torch.ones(5))).cuda(), tokens, S.new_sample_workspace(3, 5000),
+                 top_k=torch.full((8,), 40, dtype=torch.int32, device="cuda"), probs=probs)
+    torch.cuda.synchronize()
+    assert np.array_equal(tokens[:3].cpu().numpy(), want[0]) and np.array_equal(probs[:3].cpu().numpy(), want[1])
+    assert (tokens[3:] == -9).all() and (probs[3:] == 5.0).all()
