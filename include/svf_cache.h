@@ -44,7 +44,7 @@ extern "C" {
 
 typedef struct svf_chunk_shape {
   int32_t B;                 /* sequences in the batch, 1..4096                               */
-  int32_t Hq, Hkv;           /* query heads, KV heads; Hq % Hkv == 0, Hq / Hkv <= 256             */
+  int32_t Hq, Hkv;           /* query heads, KV heads; Hq % Hkv == 0, Hq <= 4096, Hq / Hkv <= 256 */
   int32_t d;                 /* head dimension: 64 or 128                                     */
   int32_t dtype;             /* SVF_F32 or SVF_BF16                                           */
   int32_t page_size;         /* tokens per physical page; 0 = contiguous cache                */

@@ -155,3 +155,13 @@ def test_sampling_arguments_have_the_types_and_sizes_that_are_read():
                 call(**{n: torch.stack((x, x), -1)[..., 0]})
     with pytest.raises(ValueError, match="probs"):
         call(probs=torch.zeros(R, V - 1))
+
+
+def test_shapes_at_the_limits():
+    for kw in (dict(max_new=1 << 22), dict(n_rows=1 << 28), dict(max_seq_len=1 << 30, page_size=0, n_pages=2), dict(Hq=4096, Hkv=4096), dict(B=4096),
+               dict(Hq=512, Hkv=2), dict(kv_strides=((1 << 34) - 8, 256, 128)), dict(kv_strides=(4096, (1 << 34) - 8, 128)),
+               dict(kv_strides=(4096, 256, (1 << 34) - 8)), dict(window=(1 << 31) - 1), dict(rotary_dim=128)):
+        assert S.svf_chunk_workspace_bytes(good(**kw)) > 0, kw
+    for kw in (dict(max_new=(1 << 22) + 1), dict(n_rows=(1 << 28) + 1), dict(Hq=4100, Hkv=4100), dict(kv_strides=(1 << 34, 256, 128)),
+               dict(kv_strides=(4096, 1 << 34, 128)), dict(kv_strides=(4096, 256, 1 << 34))):
+        assert both(good(**kw)) == -2, kw
