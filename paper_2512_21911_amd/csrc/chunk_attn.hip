@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kKeys = 64;                                // keys of a unit: 2 us
 constexpr int kExtra = 4;                                // an item's beginning and end: 8 us
-constexpr int kJoin = 16;                                // what cutting costs: a second beginning and the merge (2048 tokens over 32k: 962 us cut, 933 not)
 
 template <int D>
 struct Kernel {
@@ -33,6 +32,10 @@ struct Kernel {
   static constexpr int kRowsPerPass = kThreads / kChunks;
   static constexpr int kPasses = kKeys / kRowsPerPass;
   static constexpr int kLds = 8 * kTileBytes;            // four units; at first the sums over the sequences
+  // What cutting costs, a second beginning and the merge.  Cut and not, us, by the shares that the largest of 256 items has above the mean (8 x 256 tokens
+  // over 1000 .. 7000, 32 heads): d = 128 10: 169, 147; 25: 168, 161; 33: 169, 170; 49: 174, 188; d = 64 10: 101, 95; 18: 102, 104; 25: 101, 111.  One
+  // prompt of 2048 over 30k, 16: 940, 928 and 573, 590; of 1024 over nothing, 128 items, 14: 48, 39 and 33, 28.
+  static constexpr int kJoin = D == 128 ? 24 : 14;
   static_assert((kMostB + 1) * 8 <= kLds, "");
 
   // K chunk c of key t at c ^ (t mod 16) (d = 64, two rows to a line of banks: c ^ (t / 2 mod 8)): sixteen lanes that read the same chunk of
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
     return at;
   };
   Cursor c;
-  if (!cursor_of_few<R, kKeys, kExtra, kJoin>(p, begin, take, c)) {
+  if (!cursor_of_few<R, kKeys, kExtra, C::kJoin>(p, begin, take, c)) {
     int64_t* const cum = reinterpret_cast<int64_t*>(lds);
     units_before<R, kKeys, kExtra>(p, cum);
     begin(cum[p.B]);

@@ -78,7 +78,9 @@ struct FewBf16 {
   static constexpr int kOwn = 2 * kTileBytes;
   static constexpr int kLanesRows = 64 / kChunks, kPasses = kFewKeys / kLanesRows;      // rows that a wavefront loads at once
   static constexpr int kQueries = 16;                    // (bytes of LDS for the queries: none)
-  static constexpr int kJoin = 8;                        // what cutting costs (32 tokens, 8 KV heads over 1000 .. 1250: 39.8 us cut, 35.4 not)
+  // What cutting costs.  Cut and not, us, by the shares that the largest item has above the mean (32 and 31 tokens, 8 KV heads over 3300 .. 4700):
+  // d = 128 4: 107, 103; 15: 107, 106; 19: 106, 102; 22: 109, 110; 26: 106, 104; d = 64 4: 58, 54; 15: 57, 55; 19: 56, 52; 22: 56, 57; 26: 55, 53.
+  static constexpr int kJoin = 20;
   static constexpr int kExtra = 4;                       // an item's beginning and end, 3 us, in units of 0.8 us
   // (where a chunk of a row sits: as in the kernel for many rows)
   static __device__ __forceinline__ uint32_t k_at(int t, int c) {
@@ -169,7 +171,9 @@ struct FewF32 {
   static constexpr int kOwn = kFewKeys * kRowBytes;
   static constexpr int kLanesRows = 64 / kChunks, kPasses = kFewKeys / kLanesRows;
   static constexpr int kQueries = kFewRows * kRowBytes;
-  static constexpr int kJoin = 16;                       // (8 x 128 tokens, 8 heads over 600: 73 us cut, 49 not; d = 64 33, 24)
+  // What cutting costs.  Cut and not, us (8 x 128 tokens over 100 .. 1300, and one prompt of 800 and 900 over 1000): d = 128 5: 73, 55; 15: 76, 64;
+  // 20: 91, 87; 21: 77, 73; 24: 81, 85; d = 64 5: 34, 27; 15: 34, 31; 20: 44, 42; 21: 34, 35; 24: 39, 42.
+  static constexpr int kJoin = 22;
   static constexpr int kExtra = 8;                       // ... in units of 0.6 us (d = 64) and 1.1 us
   floatx4 k[D / 8];
   Places<1> at;                                          // (of key lane mod 32)
