@@ -28,7 +28,11 @@ HIPCC_FLAGS = [
 # Kernels that must not use scratch memory (a private segment makes every dispatch slower, and an
 # array the compiler moved there turns register accesses into memory round trips).
 NO_SCRATCH = ("verify_attn_mfma_kernel", "verify_attn_mfma_rows_kernel", "retrieve_only_kernel", "verify_attn_f32_kernel",
-              "retrieve_kernel")
+              "retrieve_kernel", "append_kv_kernel", "chunk_attn_kernelILi64", "chunk_attn_few_kernelILi64", "chunk_merge_kernel",
+              "sample_row_kernel", "sample_stats_kernel", "sample_gather_kernel", "sample_draw_kernel", "sample_probs_kernel")
+# Attention of new tokens at d = 128 has all registers in use inside its loop over the keys, and keeps what only an item's beginning
+# and end need in scratch memory: kernel -> most bytes a lane (68, 48 and 200 as built; none is touched inside that loop).
+SOME_SCRATCH = {"chunk_attn_kernelILi128": 72, "chunk_attn_few_kernelILi128ENS0_7FewBf16": 64, "chunk_attn_few_kernelILi128ENS0_6FewF32": 208}
 
 
 def hipcc_path() -> str:
@@ -60,9 +64,10 @@ def build_lib(verbose: bool = True) -> str:
     for l in remarks:
         if "Function Name:" in l:
             name = l.split("Function Name:")[1].split("[-Rpass")[0].strip()
-        elif "ScratchSize [bytes/lane]:" in l and name and any(k in name for k in NO_SCRATCH):
+        elif "ScratchSize [bytes/lane]:" in l and name:
             size = int(l.split("ScratchSize [bytes/lane]:")[1].split()[0])
-            if size != 0:
+            most = 0 if any(k in name for k in NO_SCRATCH) else next((n for k, n in SOME_SCRATCH.items() if k in name), size)
+            if size > most:
                 raise RuntimeError(f"{name} uses {size} bytes of scratch memory per lane")
     build_calls(verbose)
     return LIB_PATH
