@@ -151,7 +151,8 @@ int svf_chunk_attn(const svf_chunk_shape_t* shape, const void* q, const void* K,
   p.max_seq_len = shape->max_seq_len;
   p.max_new = shape->max_new;
   p.n_rows = shape->n_rows;
-  p.window = shape->window;
+  // (one that reaches past every sequence is none: the kernels take places less a window as 32-bit numbers)
+  p.window = shape->window >= shape->max_seq_len ? 0 : shape->window;
   // (items of 32 rows, units of 32 keys, no more than sixteen shares beside them; up to 2^24 of both each: no overflow below 2^62)
   const int64_t share_items = ((int64_t)shape->max_new * p.G + 31) / 32, share_units = (int64_t)shape->max_seq_len / 32 + 18;
   p.share_bound = share_items > (1 << 30) / share_units ? INT64_MAX : (int64_t)shape->B * shape->Hkv * share_items * share_units;

@@ -333,3 +333,17 @@ def test_large_values_under_rising_scores(dtype, d, rise):
     x["q"] = torch.ones_like(x["q"])
     x["V"] = (x["V"].clamp(-4, 4) * 2.0 ** 112).to(dtype)  # 4 x 2^112 x (940 + 64) < 2^125
     check(sh, x)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 2, (1 << 31) - 200, 1 << 30])
+def test_windows_of_any_size(dtype, window):
+    """A window that no sequence fills is none."""
+    for lens, news, Hq, Hkv in (([0], [300], 8, 2), ([50, 0], [700, 3], 2, 2), ([0, 900, 7], [1, 1, 1], 8, 2)):
+        sh, x = build(lens, news, dtype=dtype, Hq=Hq, Hkv=Hkv, d=64)
+        g = to_gpu(x)
+        want, want_lse = call(sh, g)
+        sh.window = window
+        out, lse = call(sh, g)
+        verify(sh, x, out, lse)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
