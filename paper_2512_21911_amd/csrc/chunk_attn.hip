@@ -6,12 +6,13 @@
 // lane mod 32: row statistics are a lane's own but for one exchange of halves, and the weights, rounded to bf16, are the second
 // product's operand where they are.  The rounding is the size of the output's own, 2^-8 of a weight at most, and l is summed from the unrounded ones.
 //
-// Bound by the matrix cores: 2048 tokens over 32k, 32 heads, d = 128: 943 us, 1.13 PFLOP/s, where a bf16 product of 8192^3 in the library reaches
-// 1.27.  At d = 64 there are two weights to work out for every four products and the exponentials bind (a quarter of the rate of other vector
-// instructions): 345 TFLOP/s with windows of 1024.  What it took, from 1461 us with all wavefronts in step: two of a SIMD a phase apart, one multiplies
+// 2048 tokens over 32k, 32 heads, d = 128: 921 to 977 us, 1.09 to 1.15 PFLOP/s, where a bf16 product of 8192^3 in the library reaches 1.27.  Matrix cores and vector
+// units are busy 63 and 62 % of the cycles, and the clock gives way to them.  At d = 64 there are two weights to work out for every four products: 0.91 PFLOP/s
+// for 2048 over 30k; with windows of 1024 (288 items, 350 TFLOP/s) they are busy 25 and 50 %, and the beginnings and ends of items are
+// the rest.  What it took for the first, from 1461 us with all wavefronts in step: two of a SIMD a phase apart, one multiplies
 // while the other works out weights (1220), operands read four products ahead, places without divisions, a head's ranges on one XCD (1163), no
 // maximum per unit (1116), loading between the two products (1017), ranges by cost and masks by one comparison (960), items not cut where each has a
-// workgroup (943).
+// workgroup (943 then).
 #include <algorithm>
 
 #include "chunk_share.h"
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkParams p) 
       outputs(u);
       if (u + 3 < n) {
         // Loading, in the products' shadow: unit u + 3 into LDS (both have multiplied by the values of unit u - 1, which were there), u + 4
-        // on its way, u + 5 looked up.  (One place for all three: 957 us for 2048 tokens over 32k; among the first products 977, spread
+        // on its way, u + 5 looked up.  (One place for all three: 957 us then for 2048 tokens over 32k; among the first products 977, spread
         // over the outputs 1179, while the weights are worked out 1116.)
         put((u + 3) & 3, on_way);
         if (u + 4 < n) {

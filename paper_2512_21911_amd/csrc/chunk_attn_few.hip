@@ -5,8 +5,8 @@
 // The eight wavefronts of a workgroup have nothing to do with one another until the end of an item: each takes every eighth unit of 32 keys, the
 // next unit's loads on their way while one is worked on, and keeps its own maximum, sum and output.  Then the eight are joined through LDS, and where an
 // item was cut, the last of its workgroups joins the parts.
-//   bf16  bound by memory, the cache goes by once, 128 KB in flight on a compute unit at d = 128: 537 MB for four tokens over 32k in 109 us,
-//         4.9 TB/s (one token over 8k, 34 MB: 17 us, of which launch, first tiles and join are 10).  The matrix cores still do both products (32 rows
+//   bf16  bound by memory, the cache goes by once, 128 KB in flight on a compute unit at d = 128: 537 MB for four tokens over 32k in 111 us,
+//         4.8 TB/s (one token over 8k, 34 MB: 17 us, of which launch, first tiles and join are 10).  The matrix cores still do both products (32 rows
 //         at a time, whatever of them is used), and have the time for weights of sixteen bits (two bf16 terms): what is left of a weight behind
 //         its first term is rounded to bf16 too, 2^-16 of the weight.
 //   fp32  bound by the fp32 matrix instructions (v_mfma_f32_32x32x2_f32: 64 cycles per 4096 operations, 157 TFLOP/s over the chip; 32 keys in

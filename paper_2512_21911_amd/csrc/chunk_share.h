@@ -207,7 +207,8 @@ __device__ __forceinline__ int shares_upto(const ChunkParams& p, const ChunkSeq&
 }
 
 // The same without LDS and barriers, by every wavefront for itself, for up to 64 sequences (lane b has sequence b) and groups of a power of two
-// of query heads, whose items' units have a sum in closed form.  `begin` says where the range begins, given the total.  JOIN: shares that the end of an
+// of query heads, whose items' units have a sum in closed form (64 single tokens over 1000 57 us, 65 by the other way 61; one token over 8000 for groups of
+// eight query heads 17.5 us, of seven 18.8; 2048 over 30k 1.16 and 1.10 PFLOP/s).  `begin` says where the range begins, given the total.  JOIN: shares that the end of an
 // item costs if it was cut; where no more workgroups than there are have an item each, and the largest is within that of an equal range, they aren't
 // cut (JOIN = 0: always); `take` says which, given how many there are.
 template <int R, int KEYS, int EXTRA, int JOIN, typename Begin, typename Take>

@@ -3,8 +3,8 @@
 // All three filters keep a prefix of the tokens in descending order of their logits (ties by index), so what a row keeps
 // is two numbers, a border: the last kept logit and the index of the last kept token with it.  Nothing is sorted but the few tokens around it.
 // A row is cut into slices of up to 32 768 logits, which a workgroup holds in registers, and three steps find border and token:
-//   stats    of a slice: the maximum and the sum of the weights or, if the row has a filter, a histogram of counts and weights over 1023 bins of
-//            logits from the maximum down.
+//   stats    of a slice: the maximum and the sum of the weights or, if the row has a filter, a histogram of counts and weights over 1024 bins of
+//            logits from the maximum down (those further down are counted and weighed together).
 //   gather   the row's histograms are added up, and the bin is known that the border is in; the tokens in it go to the row's list (top-k: all from
 //            the top on, so that the mass that top-p takes its share of is at hand).
 //   draw     the list is sorted and walked to the border, what every slice keeps is added up, and the token is found: by the
@@ -13,7 +13,8 @@
 // three: a workgroup per slice, per slice (which reads its slice again if it has tokens for the list), per row.  A fourth, with a workgroup per
 // slice again, writes the probabilities where they are asked for.
 // A row whose border bin has more tokens than the list (many equal logits, a top-k of thousands) is settled in the third step by
-// radix selection over the whole row.
+// radix selection over the whole row, by its one workgroup: equal logits with top-p 0.9 0.23 ms (32 000) and 0.66 (129 280), nearly equal ones 0.13 and 0.32, a
+// top-k of 5000 0.10 and 0.26, with top-p 0.17 and 0.45.  Temperatures above two weigh what is below the bins in fp64: 33 us instead of 25 with top-p.
 //
 // Weights.  Bins are a power of two of logits wide, at whole multiples of it, so a logit's bin and its place in the bin are exact in fp32.  A
 // weight is its bin's, 2^(-bin c) in fp64, times 2^(place c), place c < 0.046: a short polynomial in fp32 whose rounding is 2^-24 of the
@@ -40,7 +41,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kFraction = 43;                            // bits of a weight behind the point; 2^19 weights of 1.05 fit 63 bits
 constexpr int kPlaceBits = 31;                           // of a weight relative to its bin's: at least one, below two
 constexpr int kCountAt = 47;                             // a histogram's word: what 2^15 such weights have over one, and above that how many
-constexpr int kBins = 1024;                              // the last: everything below the others
+constexpr int kBins = 1024;                              // from the maximum's down; logits further down are in none
 constexpr int kList = 4096;                              // tokens around the border that are sorted
 constexpr float kFar = 3e38f;                            // bins of logits further from zero are this one
 constexpr double kLog2e = 1.4426950408889634074;
@@ -154,7 +155,7 @@ struct Settings {
     if (k >= p.V || k < 0) k = 0;
     if (!(top_p < 1.f)) top_p = 1.f;
     if (!(min_p > 0.f)) min_p = 0.f;
-    // a bin is 1/32 of a logit wide, and of the temperature's power of two if that is lower: the 1023 bins reach 32 logits, or 16
+    // a bin is 1/32 of a logit wide, and of the temperature's power of two if that is lower: the 1024 bins reach 32 logits, or 16
     // to 32 temperatures, below the maximum
     const int e = min(0, (int)((__float_as_uint(temperature) >> 23) & 255) - 127);
     per_bin = __uint_as_float((uint32_t)(127 + 5 - e) << 23);

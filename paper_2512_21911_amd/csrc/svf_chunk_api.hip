@@ -54,7 +54,7 @@ svf::KvLayout layout_of(const svf_chunk_shape_t& s) {
 }
 
 // The choice between the kernels: the one for few rows takes 32 at a time and keeps memory busier, which binds where rows are few.  Four sequences of
-// 32k, one token of four heads a KV head: 109 us against 169 by the other; nine tokens, whose 36 rows it reads the keys twice for: 203 against 149.
+// 32k, one token of four heads a KV head: 111 us against 169 by the other; nine tokens, whose 36 rows it reads the keys twice for: 203 against 150.
 bool few_rows(const svf_chunk_shape_t& s) { return s.dtype == SVF_F32 || svf::chunk_attn_is_few(s.Hq / s.Hkv, s.max_new); }
 
 size_t workspace_of(const svf_chunk_shape_t& s) {
