@@ -83,7 +83,8 @@ size_t svf_sample_workspace_bytes(int32_t rows, int32_t V);
  * weight zero, NaN counts as -inf; a row of nothing else gets token -1 and probabilities of zero.
  * A weight is good to 2^-27 of itself (where it is below e^-16 of the largest: 2^-18), and top_p and the draw count in units of 2^-43 of the largest;
  * sums are of whole numbers or in 64 bits in a fixed order: the same bits from call to call.
- * A temperature below 2^-60 counts as that; logits further than 2^122 from zero (temperatures below one: 2^122 temperatures) weigh as those there.
+ * A temperature below 2^-60 counts as that; logits further than 2^120 from zero (temperatures below one: 2^120 temperatures) may
+ * weigh as those there.
  * Time: rows whose border is among more than 4096 tokens within 1/32 of a logit (flat logits, many equal ones), or whose top_k is above 4096, are gone over several
  * times by one workgroup: 0.25 to 0.7 ms for 129 280 logits where others take 0.02 to 0.04, whatever else the rows of the call are.
  * SVF_ERR_DTYPE, SVF_ERR_NULL, SVF_ERR_SHAPE (rows, V, a stride below V, pointers that are not aligned to their elements), SVF_ERR_WORKSPACE.

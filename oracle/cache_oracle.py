@@ -69,6 +69,7 @@ def kept(x, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     top = x[order[0]]
     with np.errstate(invalid="ignore"):
         z = np.where(x == top, 0.0, (x - top) / temperature)
+    z = np.where((x == -np.inf) & (top > -np.inf), -np.inf, z)      # (whatever the temperature)
     w = np.exp(z)
     if top_k > 0:
         order = order[:top_k]

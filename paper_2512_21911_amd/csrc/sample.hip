@@ -43,7 +43,7 @@ constexpr int kPlaceBits = 31;                           // of a weight relative
 constexpr int kCountAt = 47;                             // a histogram's word: what 2^15 such weights have over one, and above that how many
 constexpr int kBins = 1024;                              // from the maximum's down; logits further down are in none
 constexpr int kList = 4096;                              // tokens around the border that are sorted
-constexpr float kFar = 3e38f;                            // bins of logits further from zero are this one
+constexpr float kFar = 1.5e38f;                          // bins of logits further from zero are this one (twice as many have a number)
 constexpr double kLog2e = 1.4426950408889634074;
 
 struct SliceStats {

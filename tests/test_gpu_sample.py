@@ -264,3 +264,14 @@ def test_buffers_longer_than_the_batch():
     torch.cuda.synchronize()
     assert np.array_equal(tokens[:3].cpu().numpy(), want[0]) and np.array_equal(probs[:3].cpu().numpy(), want[1])
     assert (tokens[3:] == -9).all() and (probs[3:] == 5.0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [90, 9000, 40000])
+def test_no_temperature_tells_the_largest_from_the_lowest(dtype, V):
+    # at an infinite temperature all tokens but those of -inf weigh the same, however far apart
+    lg, u = rows(5, V, seed=V, dtype=dtype)
+    lg[:, 1::3], lg[:, 5::40], lg[:, 7::50] = torch.finfo(dtype).min, torch.finfo(dtype).max, -float("inf")
+    inf = float("inf")
+    check(lg, u, temperature=[inf] * 5)
+    check(lg, u, temperature=[inf] * 5, top_p=[0.5, 0.9, 1.0, 0.7, 0.01], top_k=[0, 0, V // 2, 40, V - V // 7])
